@@ -337,6 +337,94 @@ int32_t ef21_last_path(const ef21_ctx* ctx);
 /* Kernel launches enqueued by this handle since creation (host copies are not counted). */
 int64_t ef21_launch_count(const ef21_ctx* ctx);
 
+/* ---------------------------------------------------------------------------------------------
+ * Objectives of a language model's worker, and the sparse end of its gradient
+ *
+ * The vectors that ef21_step_grads takes come from a model.  For a language model these calls are both of its ends: the rows of
+ * its embedding table and the table's gradient; and, from its logits on, what it is trained on -- log-probabilities of tokens, the
+ * logistic loss of paired log ratios (the logistic loss of Section 5 with a pair's log ratio as the margin), a clipped policy loss, and the balance
+ * loss of a router that is added to either -- each with its gradient.  Tensors may be fp32, bfloat16 or half; sums, softmax
+ * statistics and losses are fp32 or fp64, results are rounded once, in a fixed order: repeated runs agree bit for bit.
+ * Strides and offsets are in elements, the last dimension is contiguous; no call holds state, and two calls whose workspaces
+ * and outputs are not shared may run at the same time.  Device pointers belong to the current device.  mask arrays hold one byte per entry: not 0 = counts;
+ * what a mask leaves out may hold anything, NaN too.
+ * --------------------------------------------------------------------------------------------- */
+enum { EF21_DTYPE_F32 = 0, EF21_DTYPE_BF16 = 1, EF21_DTYPE_F16 = 2 };
+enum { EF21_INDEX_I32 = 0, EF21_INDEX_I64 = 1 };
+enum {
+    EF21_REDUCE_TOKENS = 0,   /* every token that counts weighs the same */
+    EF21_REDUCE_SEQUENCES = 1 /* every row with such tokens weighs the same, its tokens alike */
+};
+
+/* Log-probabilities of given tokens: lse = log sum_j exp(scale x_j), logp = scale x_target - lse, for `batch` times `length` rows of
+ * `vocab` logits; row (b, t) starts at b batch_stride + t row_stride, its target is targets[b targets_batch_stride + t].
+ * logps_out and lse_out: [batch][length].  scale > 0 (one over a temperature).  A row whose target is `ignore` is not read: 0 and 0.
+ * A target outside [0, vocab): NaN and NaN.  A row of -inf only: -inf and -inf.  +inf or NaN among the logits: NaN. */
+ef21_status ef21_token_logprobs(const void* logits_dev, int32_t dtype, int64_t batch, int64_t length, int64_t vocab,
+                                int64_t batch_stride, int64_t row_stride, const void* targets_dev, int32_t index_type,
+                                int64_t targets_batch_stride, float scale, int64_t ignore, float* logps_out_dev,
+                                float* lse_out_dev, void* cuda_stream);
+/* The logits' gradient, given that of the log-probabilities (grad_dev[batch][length]) and the forward pass's lse_dev:
+ * out_j = scale grad (1[j = target] - exp(scale x_j - lse)), in the logits' type.  out may be the logits themselves (same strides), or must not
+ * overlap them.  Rows that are ignored, whose grad is 0, or whose lse is -inf get zeros and are not read. */
+ef21_status ef21_token_logprobs_grad(const void* logits_dev, int32_t dtype, int64_t batch, int64_t length, int64_t vocab,
+                                     int64_t batch_stride, int64_t row_stride, const void* targets_dev, int32_t index_type,
+                                     int64_t targets_batch_stride, const float* lse_dev, const float* grad_dev, float scale,
+                                     int64_t ignore, void* out_dev, int64_t out_batch_stride, int64_t out_row_stride,
+                                     void* cuda_stream);
+
+/* Preference loss.  logps, ref (NULL: 0) and mask (NULL: all count) are [2 pairs][length]: the chosen answers, then the
+ * rejected ones.  s_r = sum_t mask (logps - ref), z_p = beta (s_p - s_{pairs+p}),
+ *     loss = 1/norm sum_p [ -(1 - smoothing) log sigma(z_p) - smoothing log sigma(-z_p) ]
+ * rewards_out[2 pairs] = beta s_r; grad_out[2 pairs][length] = d loss / d logps, in logps' type.  norm > 0 (usually `pairs`; more where a
+ * step's pairs come in several calls). */
+size_t ef21_preference_loss_workspace_bytes(int64_t pairs, int64_t length);
+ef21_status ef21_preference_loss(const void* logps_dev, const void* ref_dev, const uint8_t* mask_dev, int32_t dtype,
+                                 int64_t pairs, int64_t length, int64_t logps_stride, int64_t ref_stride, int64_t mask_stride,
+                                 double beta, double smoothing, double norm, float* loss_out_dev, float* rewards_out_dev,
+                                 void* grad_out_dev, void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+
+/* Clipped policy loss with a KL term, over [rows][length] tokens: with d = logps - old, r = exp(d), delta = ref - logps,
+ *     loss = sum w ( -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_weight (exp(delta) - delta - 1) )
+ * A = advantages[row][t] (advantages_per_token) or advantages[row advantages_stride]; w = 0 where the mask leaves a token out, else 1 / norm
+ * (EF21_REDUCE_TOKENS) or 1 / (norm * tokens of the row) (EF21_REDUCE_SEQUENCES).  norm = 0: the tokens that count, or the rows that have
+ * any, are counted; otherwise the caller's (all tokens, or rows, of a step that comes in several calls).  ref may be NULL where kl_weight is 0.
+ * terms_out[4]: the loss, its policy term, the KL term before its weight, and the share of clipped tokens (A > 0 and r > 1 + clip_high, or
+ * A < 0 and r < 1 - clip_low), all weighted by w.  grad_out[rows][length] = d loss / d logps, in logps' type; no token at all: zeros. */
+size_t ef21_policy_loss_workspace_bytes(int64_t rows, int64_t length);
+ef21_status ef21_policy_loss(const void* logps_dev, const void* old_dev, const void* ref_dev, const void* advantages_dev,
+                             const uint8_t* mask_dev, int32_t dtype, int64_t rows, int64_t length, int64_t logps_stride,
+                             int64_t old_stride, int64_t ref_stride, int64_t advantages_stride, int64_t mask_stride,
+                             int32_t advantages_per_token, double clip_low, double clip_high, double kl_weight,
+                             int32_t reduction, double norm, float* terms_out_dev, void* grad_out_dev, void* workspace_dev,
+                             size_t workspace_bytes, void* cuda_stream);
+
+/* Balance loss of a router over `rows` tokens and up to 1,024 experts.  choices[rows][chosen]: the experts each token goes to (one outside
+ * [0, experts) counts for none); mask[rows] (NULL: all count).  With p = softmax(logits), N the tokens that count, counts_e those that chose e:
+ *     f_e = counts_e / (chosen N),  P_e = 1/N sum_t p_te,  loss = weight experts sum_e f_e P_e
+ * counts_out[experts], probs_out[experts] = P, grad_out[rows][experts] = d loss / d logits in the logits' type (the choices are constants).
+ * Rows that do not count, and rows of -inf only, have p = 0 and a gradient of 0.  No token at all: zeros. */
+size_t ef21_balance_loss_workspace_bytes(int64_t rows, int64_t experts);
+ef21_status ef21_balance_loss(const void* logits_dev, int32_t dtype, int64_t rows, int64_t experts, int64_t logits_stride,
+                              const void* choices_dev, int32_t index_type, int64_t chosen, int64_t choices_stride,
+                              const uint8_t* mask_dev, double weight, float* loss_out_dev, int32_t* counts_out_dev,
+                              float* probs_out_dev, void* grad_out_dev, void* workspace_dev, size_t workspace_bytes,
+                              void* cuda_stream);
+
+/* out[count][dim] = scale weight[tokens[t]], in the table's type; a token outside [0, vocab) reads as zeros (as where a table
+ * is split by rows). */
+ef21_status ef21_embedding(const void* weight_dev, int32_t dtype, int64_t vocab, int64_t dim, int64_t weight_stride,
+                           const void* tokens_dev, int32_t index_type, int64_t count, float scale, void* out_dev,
+                           void* cuda_stream);
+/* The table's gradient: out[v] = scale * sum of grad[t] over the positions t with tokens[t] = v, added up in fp32 in an order that depends on
+ * the tokens alone, rounded once; accumulate: out[v] += the same, rows that no token names are not touched (otherwise they are zeros).  Tokens outside
+ * [0, vocab) and those equal to `padding` (-1: none) add nothing.  out is [vocab][dim] in grad's type or fp32. */
+size_t ef21_embedding_grad_workspace_bytes(int64_t count, int64_t vocab, int64_t dim);
+ef21_status ef21_embedding_grad(const void* grad_dev, int32_t dtype, int64_t count, int64_t dim, int64_t grad_stride,
+                                const void* tokens_dev, int32_t index_type, int64_t vocab, int64_t padding, float scale,
+                                void* out_dev, int32_t out_dtype, int64_t out_stride, int32_t accumulate,
+                                void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

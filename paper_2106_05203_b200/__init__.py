@@ -8,7 +8,9 @@ __all__ = ["binding", "build"]
 def __getattr__(name):
     if name in ("EF21", "topk", "Ef21Error", "workspace_bytes", "status_string",
                 "INIT_COMPRESSED", "INIT_ZERO", "INIT_GRADIENT",
-                "PATH_AUTO", "PATH_LAUNCHES", "PATH_PERSISTENT"):
+                "PATH_AUTO", "PATH_LAUNCHES", "PATH_PERSISTENT",
+                "token_logprobs", "token_logprobs_grad", "preference_loss", "policy_loss", "balance_loss", "embedding", "embedding_grad",
+                "PreferenceLoss", "PolicyLoss", "BalanceLoss"):
         from . import binding
         return getattr(binding, name)
     raise AttributeError(name)

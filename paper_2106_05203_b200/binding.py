@@ -12,7 +12,7 @@ import functools
 import importlib.util
 import os
 import warnings
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import numpy as np
 import torch
@@ -32,7 +32,7 @@ VARIANT_EF21, VARIANT_EF21_PLUS, VARIANT_EF = 0, 1, 2
 OBJECTIVE_LOGISTIC, OBJECTIVE_LEAST_SQUARES = 0, 1
 
 # name -> (restype, argtypes); mirrors include/ef21.h
-_i32, _i64, _f32, _sz, _vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t, ctypes.c_void_p
+_i32, _i64, _f32, _f64, _sz, _vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_double, ctypes.c_size_t, ctypes.c_void_p
 _dp = ctypes.POINTER(ctypes.c_double)
 SIGNATURES = {
     "ef21_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -76,6 +76,18 @@ SIGNATURES = {
     "ef21_set_path": (ctypes.c_int, [_vp, _i32]),
     "ef21_last_path": (_i32, [_vp]),
     "ef21_launch_count": (_i64, [_vp]),
+    "ef21_token_logprobs": (ctypes.c_int, [_vp, _i32, _i64, _i64, _i64, _i64, _i64, _vp, _i32, _i64, _f32, _i64, _vp, _vp, _vp]),
+    "ef21_token_logprobs_grad": (ctypes.c_int, [_vp, _i32, _i64, _i64, _i64, _i64, _i64, _vp, _i32, _i64, _vp, _vp, _f32, _i64, _vp, _i64, _i64, _vp]),
+    "ef21_preference_loss_workspace_bytes": (_sz, [_i64, _i64]),
+    "ef21_preference_loss": (ctypes.c_int, [_vp, _vp, _vp, _i32, _i64, _i64, _i64, _i64, _i64, _f64, _f64, _f64, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "ef21_policy_loss_workspace_bytes": (_sz, [_i64, _i64]),
+    "ef21_policy_loss": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _i32, _i64, _i64, _i64, _i64, _i64, _i64, _i64, _i32, _f64, _f64, _f64, _i32, _f64,
+                                        _vp, _vp, _vp, _sz, _vp]),
+    "ef21_balance_loss_workspace_bytes": (_sz, [_i64, _i64]),
+    "ef21_balance_loss": (ctypes.c_int, [_vp, _i32, _i64, _i64, _i64, _vp, _i32, _i64, _i64, _vp, _f64, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "ef21_embedding": (ctypes.c_int, [_vp, _i32, _i64, _i64, _i64, _vp, _i32, _i64, _f32, _vp, _vp]),
+    "ef21_embedding_grad_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "ef21_embedding_grad": (ctypes.c_int, [_vp, _i32, _i64, _i64, _i64, _vp, _i32, _i64, _i64, _f32, _vp, _i32, _i64, _i32, _vp, _sz, _vp]),
 }
 
 
@@ -439,3 +451,337 @@ def topk_static(v: torch.Tensor, k: int, idx: torch.Tensor, val: torch.Tensor,
     with torch.cuda.device(v.device):
         _check(_lib.ef21_topk_static(_ptr(v), batch, d, k, _ptr(idx), _ptr(val), _stream_handle(stream)),
                "ef21_topk_static")
+
+
+# -- objectives of a language model's worker, and the sparse end of its gradient ------------------------------------------------------
+# Every call works on the current stream of its tensors' device, or on `stream`: outputs and workspace then belong to that stream, and the
+# caller orders it behind what made the inputs.  Results are constants to torch's autograd; a gradient goes on with tensor.backward(gradient).
+
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+INDEX_TYPES = {torch.int32: 0, torch.int64: 1}
+REDUCTIONS = {"token": 0, "sequence": 1}
+
+
+class PreferenceLoss(NamedTuple):
+    loss: torch.Tensor          # fp32, one number
+    rewards: torch.Tensor       # fp32 [2 P]: beta times every row's log ratio
+    grad: torch.Tensor          # [2 P, T]: of logps, in its type
+
+
+class PolicyLoss(NamedTuple):
+    terms: torch.Tensor         # fp32 [4]: the loss, its policy term, the KL term before its weight, the share of clipped tokens
+    grad: torch.Tensor          # [R, T]: of logps, in its type
+
+
+class BalanceLoss(NamedTuple):
+    loss: torch.Tensor          # fp32, one number
+    counts: torch.Tensor        # int32 [E]: tokens per expert
+    probs: torch.Tensor         # fp32 [E]: mean probabilities
+    grad: torch.Tensor          # [R, E]: of the logits, in their type
+
+
+def _type_of(t: torch.Tensor, name: str) -> int:
+    code = DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, not {t.dtype}")
+    return code
+
+
+def _index_type_of(t: torch.Tensor, name: str) -> int:
+    code = INDEX_TYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be int32 or int64, not {t.dtype}")
+    return code
+
+
+def _last_contiguous(t: torch.Tensor, name: str) -> None:
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise TypeError(f"the last dimension of {name} must be contiguous")
+
+
+def _matrix(t: torch.Tensor, name: str, shape, dtype=None) -> int:
+    """The row stride of a matrix with contiguous rows."""
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be of shape {tuple(shape)}, not {tuple(t.shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    _last_contiguous(t, name)
+    return t.stride(0)
+
+
+def _mask(t: Optional[torch.Tensor], shape) -> int:
+    if t is None:
+        return 0
+    if t.dtype not in (torch.bool, torch.uint8):
+        raise TypeError(f"mask must be bool or uint8, not {t.dtype}")
+    return _matrix(t, "mask", shape)
+
+
+def _same_device(*tensors: Optional[torch.Tensor]) -> torch.device:
+    device = tensors[0].device
+    if device.type != "cuda":
+        raise TypeError("expected CUDA tensors; there is no CPU path")
+    for t in tensors[1:]:
+        if t is not None and t.device != device:
+            raise ValueError(f"tensors on {device} and on {t.device}")
+    return device
+
+
+def _elsewhere(device: torch.device, stream: Optional[torch.cuda.Stream]):
+    """None where the call's stream and device are the current ones; else the context in which they are."""
+    if stream is not None:
+        if stream.device != device:
+            raise ValueError(f"tensors on {device}, a stream of {stream.device}")
+        return torch.cuda.stream(stream)
+    return None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _workspace(nbytes: int, device: torch.device, where: str):
+    """A workspace, and its 256-byte aligned address."""
+    if nbytes == 0:
+        raise Ef21Error(1, where)
+    ws = torch.empty(nbytes + 255, dtype=torch.uint8, device=device)
+    return ws, (ws.data_ptr() + 255) // 256 * 256
+
+
+def _logit_rows(logits: torch.Tensor, name: str):
+    """(batch, length, vocab, batch stride, row stride) of a matrix of rows, or of one per batch entry; a view such as x[:, :-1] is one too."""
+    if logits.dim() == 2:
+        _last_contiguous(logits, name)
+        return 1, logits.shape[0], logits.shape[1], 0, logits.stride(0)
+    if logits.dim() != 3:
+        raise ValueError(f"{name} must be [rows, vocab] or [batch, length, vocab], not {tuple(logits.shape)}")
+    _last_contiguous(logits, name)
+    return (*logits.shape, logits.stride(0), logits.stride(1))
+
+
+def _targets_fit(targets: torch.Tensor, logits: torch.Tensor) -> None:
+    if targets.shape != logits.shape[:-1]:
+        raise ValueError(f"targets must be of shape {tuple(logits.shape[:-1])}, not {tuple(targets.shape)}")
+
+
+def _target_rows(targets: torch.Tensor):
+    """targets and their stride between batch entries; copied where those of an entry do not follow one another (eight bytes a row)."""
+    if targets.shape[-1] > 1 and targets.stride(-1) != 1:
+        targets = targets.contiguous()
+    return targets, targets.stride(0) if targets.dim() == 2 else 0
+
+
+def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, scale: float = 1.0, ignore: int = -100, stream: Optional[torch.cuda.Stream] = None):
+    """Log-probabilities of targets[...] under softmax(scale * logits[..., vocab]) -> (logps, lse), fp32, of targets' shape.
+
+    logits[rows, vocab] or [batch, length, vocab], with any strides between rows: score whole sequences as
+    token_logprobs(logits[:, :-1], tokens[:, 1:]), no copy is made.  Where the target is `ignore`, the row is not read and both are 0."""
+    dtype, index = _type_of(logits, "logits"), _index_type_of(targets, "targets")
+    batch, length, vocab, batch_stride, row_stride = _logit_rows(logits, "logits")
+    _targets_fit(targets, logits)
+    device = _same_device(logits, targets)
+    there = _elsewhere(device, stream)
+    if there is not None:
+        with there:
+            return token_logprobs(logits, targets, scale, ignore)
+    targets, target_stride = _target_rows(targets)
+    logps = torch.empty(targets.shape, dtype=torch.float32, device=device)
+    lse = torch.empty(targets.shape, dtype=torch.float32, device=device)
+    _check(_lib.ef21_token_logprobs(logits.data_ptr(), dtype, batch, length, vocab, batch_stride, row_stride, targets.data_ptr(), index, target_stride,
+                                    scale, ignore, logps.data_ptr(), lse.data_ptr(), _current_raw_stream(device.index)), "ef21_token_logprobs")
+    return logps, lse
+
+
+def token_logprobs_grad(logits: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, grad: torch.Tensor, scale: float = 1.0, ignore: int = -100,
+                        out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The logits' gradient, given that of the log-probabilities: grad[...] and lse[...] are contiguous fp32 of targets' shape, the other arguments as
+    they were for token_logprobs.  out (of logits' shape and type) may be the logits themselves, which are then overwritten."""
+    dtype, index = _type_of(logits, "logits"), _index_type_of(targets, "targets")
+    batch, length, vocab, batch_stride, row_stride = _logit_rows(logits, "logits")
+    _targets_fit(targets, logits)
+    for t, name in ((lse, "lse"), (grad, "grad")):
+        if t.shape != targets.shape:
+            raise ValueError(f"{name} must be of shape {tuple(targets.shape)}, not {tuple(t.shape)}")
+        if t.dtype != torch.float32 or not t.is_contiguous():
+            raise TypeError(f"{name} must be contiguous float32")
+    if out is not None:
+        if out.shape != logits.shape or out.dtype != logits.dtype:
+            raise ValueError("out must have the logits' shape and type")
+        if any(n > 1 and st < vocab for n, st in zip(out.shape[:-1], out.stride()[:-1])):
+            raise ValueError("rows of out overlap")
+    device = _same_device(logits, targets, lse, grad, out)
+    there = _elsewhere(device, stream)
+    if there is not None:
+        with there:
+            return token_logprobs_grad(logits, targets, lse, grad, scale, ignore, out)
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=device)
+    _, _, _, out_batch_stride, out_row_stride = _logit_rows(out, "out")
+    targets, target_stride = _target_rows(targets)
+    _check(_lib.ef21_token_logprobs_grad(logits.data_ptr(), dtype, batch, length, vocab, batch_stride, row_stride, targets.data_ptr(), index, target_stride,
+                                         lse.data_ptr(), grad.data_ptr(), scale, ignore, out.data_ptr(), out_batch_stride, out_row_stride,
+                                         _current_raw_stream(device.index)), "ef21_token_logprobs_grad")
+    return out
+
+
+def preference_loss(logps: torch.Tensor, ref_logps: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None, beta: float = 0.1,
+                    smoothing: float = 0.0, norm: Optional[float] = None, stream: Optional[torch.cuda.Stream] = None) -> PreferenceLoss:
+    """Logistic loss of paired log ratios with its gradient: logps[2 P, T] are the log-probabilities of the chosen answers' tokens, then of the rejected
+    ones', ref_logps those under the reference (None: 0), mask[2 P, T] the tokens that count (None: all).  The loss is the sum over pairs over `norm`
+    (None: P)."""
+    dtype = _type_of(logps, "logps")
+    if logps.dim() != 2 or logps.shape[0] % 2 or logps.shape[0] == 0:
+        raise ValueError(f"logps must be [2 pairs, length], not {tuple(logps.shape)}")
+    shape = logps.shape
+    logps_stride = _matrix(logps, "logps", shape)
+    ref_stride = 0 if ref_logps is None else _matrix(ref_logps, "ref_logps", shape, logps.dtype)
+    mask_stride = _mask(mask, shape)
+    pairs, length = shape[0] // 2, shape[1]
+    device = _same_device(logps, ref_logps, mask)
+    there = _elsewhere(device, stream)
+    if there is not None:
+        with there:
+            return preference_loss(logps, ref_logps, mask, beta, smoothing, norm)
+    nbytes = int(_lib.ef21_preference_loss_workspace_bytes(pairs, length))
+    ws, ws_ptr = _workspace(nbytes, device, "ef21_preference_loss_workspace_bytes")
+    loss = torch.empty((), dtype=torch.float32, device=device)
+    rewards = torch.empty(2 * pairs, dtype=torch.float32, device=device)
+    grad = torch.empty(shape, dtype=logps.dtype, device=device)
+    _check(_lib.ef21_preference_loss(logps.data_ptr(), _ptr(ref_logps), _ptr(mask), dtype, pairs, length, logps_stride, ref_stride, mask_stride, beta, smoothing,
+                                     pairs if norm is None else norm, loss.data_ptr(), rewards.data_ptr(), grad.data_ptr(), ws_ptr, nbytes,
+                                     _current_raw_stream(device.index)), "ef21_preference_loss")
+    return PreferenceLoss(loss, rewards, grad)
+
+
+def policy_loss(logps: torch.Tensor, old_logps: torch.Tensor, advantages: torch.Tensor, mask: Optional[torch.Tensor] = None,
+                ref_logps: Optional[torch.Tensor] = None, clip_low: float = 0.2, clip_high: float = 0.2, kl_weight: float = 0.0,
+                reduction: str = "token", norm: Optional[float] = None, stream: Optional[torch.cuda.Stream] = None) -> PolicyLoss:
+    """Clipped policy loss with a KL term, with its gradient: logps[R, T], old_logps and ref_logps of the tokens under the policy, the one that drew them, and
+    the reference; advantages[R, T] per token, or [R] or [R, 1] per sequence; mask[R, T] the tokens that count (None: all).  reduction "token":
+    all of these weigh the same; "sequence": every row that has any does.  `norm` replaces their number where a step comes in several calls."""
+    dtype = _type_of(logps, "logps")
+    if logps.dim() != 2:
+        raise ValueError(f"logps must be [rows, length], not {tuple(logps.shape)}")
+    if reduction not in REDUCTIONS:
+        raise ValueError(f"reduction must be one of {tuple(REDUCTIONS)}, not {reduction!r}")
+    if norm is not None and not norm > 0:
+        raise ValueError("norm must be positive")
+    shape = logps.shape
+    rows, length = shape
+    logps_stride = _matrix(logps, "logps", shape)
+    old_stride = _matrix(old_logps, "old_logps", shape, logps.dtype)
+    ref_stride = 0 if ref_logps is None else _matrix(ref_logps, "ref_logps", shape, logps.dtype)
+    if ref_logps is None and kl_weight != 0:
+        raise ValueError("a KL term needs ref_logps")
+    if advantages.dtype != logps.dtype:
+        raise TypeError(f"advantages must be {logps.dtype}, not {advantages.dtype}")
+    per_token = 0
+    if tuple(advantages.shape) == (rows,) or tuple(advantages.shape) == (rows, 1):
+        adv_stride = advantages.stride(0)
+    else:
+        per_token = int(not (advantages.dim() == 2 and advantages.shape[1] > 1 and advantages.stride(1) == 0))
+        if per_token:
+            adv_stride = _matrix(advantages, "advantages", shape)
+        elif tuple(advantages.shape) != tuple(shape):
+            raise ValueError(f"advantages must be of shape {tuple(shape)} or {(rows,)}, not {tuple(advantages.shape)}")
+        else:
+            adv_stride = advantages.stride(0)
+    mask_stride = _mask(mask, shape)
+    device = _same_device(logps, old_logps, advantages, mask, ref_logps)
+    there = _elsewhere(device, stream)
+    if there is not None:
+        with there:
+            return policy_loss(logps, old_logps, advantages, mask, ref_logps, clip_low, clip_high, kl_weight, reduction, norm)
+    nbytes = int(_lib.ef21_policy_loss_workspace_bytes(rows, length))
+    ws, ws_ptr = _workspace(nbytes, device, "ef21_policy_loss_workspace_bytes")
+    terms = torch.empty(4, dtype=torch.float32, device=device)
+    grad = torch.empty(shape, dtype=logps.dtype, device=device)
+    _check(_lib.ef21_policy_loss(logps.data_ptr(), old_logps.data_ptr(), _ptr(ref_logps), advantages.data_ptr(), _ptr(mask), dtype, rows, length, logps_stride,
+                                 old_stride, ref_stride, adv_stride, mask_stride, per_token, clip_low, clip_high, kl_weight, REDUCTIONS[reduction],
+                                 0.0 if norm is None else norm, terms.data_ptr(), grad.data_ptr(), ws_ptr, nbytes, _current_raw_stream(device.index)), "ef21_policy_loss")
+    return PolicyLoss(terms, grad)
+
+
+def balance_loss(logits: torch.Tensor, choices: torch.Tensor, mask: Optional[torch.Tensor] = None, weight: float = 1.0,
+                 stream: Optional[torch.cuda.Stream] = None) -> BalanceLoss:
+    """Balance loss of a router, tokens per expert, and the gradient of the router's logits[R, E]: choices[R, K] are the experts that each token goes to
+    (one outside [0, E) counts for none), mask[R] the tokens that count (None: all)."""
+    dtype, index = _type_of(logits, "logits"), _index_type_of(choices, "choices")
+    if logits.dim() != 2:
+        raise ValueError(f"logits must be [rows, experts], not {tuple(logits.shape)}")
+    rows, experts = logits.shape
+    logits_stride = _matrix(logits, "logits", logits.shape)
+    if choices.dim() != 2 or choices.shape[0] != rows:
+        raise ValueError(f"choices must be [{rows}, chosen], not {tuple(choices.shape)}")
+    choices_stride = _matrix(choices, "choices", choices.shape)
+    if mask is not None and mask.dim() != 1:
+        raise ValueError(f"mask must be of shape {(rows,)}, not {tuple(mask.shape)}")
+    _mask(mask, (rows,))
+    device = _same_device(logits, choices, mask)
+    there = _elsewhere(device, stream)
+    if there is not None:
+        with there:
+            return balance_loss(logits, choices, mask, weight)
+    nbytes = int(_lib.ef21_balance_loss_workspace_bytes(rows, experts))
+    ws, ws_ptr = _workspace(nbytes, device, "ef21_balance_loss_workspace_bytes")
+    loss = torch.empty((), dtype=torch.float32, device=device)
+    counts = torch.empty(experts, dtype=torch.int32, device=device)
+    probs = torch.empty(experts, dtype=torch.float32, device=device)
+    grad = torch.empty((rows, experts), dtype=logits.dtype, device=device)
+    _check(_lib.ef21_balance_loss(logits.data_ptr(), dtype, rows, experts, logits_stride, choices.data_ptr(), index, choices.shape[1], choices_stride, _ptr(mask),
+                                  weight, loss.data_ptr(), counts.data_ptr(), probs.data_ptr(), grad.data_ptr(), ws_ptr, nbytes,
+                                  _current_raw_stream(device.index)), "ef21_balance_loss")
+    return BalanceLoss(loss, counts, probs, grad)
+
+
+def embedding(weight: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """scale * weight[tokens] -> [*tokens.shape, dim]; a token outside the table reads as zeros (as where a table is split by rows)."""
+    dtype, index = _type_of(weight, "weight"), _index_type_of(tokens, "tokens")
+    if weight.dim() != 2:
+        raise ValueError(f"weight must be [vocab, dim], not {tuple(weight.shape)}")
+    stride = _matrix(weight, "weight", weight.shape)
+    device = _same_device(weight, tokens)
+    there = _elsewhere(device, stream)
+    if there is not None:
+        with there:
+            return embedding(weight, tokens, scale)
+    tokens = tokens.contiguous()
+    out = torch.empty((*tokens.shape, weight.shape[1]), dtype=weight.dtype, device=device)
+    _check(_lib.ef21_embedding(weight.data_ptr(), dtype, weight.shape[0], weight.shape[1], stride, tokens.data_ptr(), index, tokens.numel(), scale,
+                               out.data_ptr(), _current_raw_stream(device.index)), "ef21_embedding")
+    return out
+
+
+def embedding_grad(grad: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: float = 1.0, padding: int = -1, dtype: Optional[torch.dtype] = None,
+                   out: Optional[torch.Tensor] = None, accumulate: bool = False, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The table's gradient [vocab, dim] from that of embedding(): for every token scale times the sum of grad[...] at its positions, in a fixed order.
+
+    The result is of grad's type, or float32 (dtype=torch.float32, or an fp32 out).  accumulate adds to out; the token `padding` adds nothing."""
+    code, index = _type_of(grad, "grad"), _index_type_of(tokens, "tokens")
+    if grad.dim() < 1 or tuple(grad.shape[:-1]) != tuple(tokens.shape):
+        raise ValueError(f"grad must be of shape {(*tokens.shape, 'dim')}, not {tuple(grad.shape)}")
+    if accumulate and out is None:
+        raise ValueError("accumulate needs out")
+    dim, count = grad.shape[-1], tokens.numel()
+    if grad.dim() == 2:
+        stride = _matrix(grad, "grad", grad.shape)
+    elif grad.is_contiguous():
+        stride = dim
+    else:
+        raise TypeError("grad must be a matrix with contiguous rows, or contiguous")
+    result = dtype or (grad.dtype if out is None else out.dtype)
+    if result not in (grad.dtype, torch.float32) or (out is not None and out.dtype != result):
+        raise TypeError(f"the result must be of grad's type or float32, not {result}")
+    if out is not None:
+        out_stride = _matrix(out, "out", (vocab, dim))
+        if vocab > 1 and out_stride < dim:
+            raise ValueError("rows of out overlap")
+    device = _same_device(grad, tokens, out)
+    there = _elsewhere(device, stream)
+    if there is not None:
+        with there:
+            return embedding_grad(grad, tokens, vocab, scale, padding, dtype, out, accumulate)
+    tokens = tokens.contiguous()
+    nbytes = int(_lib.ef21_embedding_grad_workspace_bytes(count, vocab, dim))
+    ws, ws_ptr = _workspace(nbytes, device, "ef21_embedding_grad_workspace_bytes")
+    if out is None:
+        out, out_stride = torch.empty((vocab, dim), dtype=result, device=device), dim
+    _check(_lib.ef21_embedding_grad(grad.data_ptr(), code, count, dim, stride, tokens.data_ptr(), index, vocab, padding, scale, out.data_ptr(), DTYPES[result],
+                                    out_stride, int(accumulate), ws_ptr, nbytes, _current_raw_stream(device.index)), "ef21_embedding_grad")
+    return out

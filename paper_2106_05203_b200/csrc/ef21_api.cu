@@ -15,6 +15,7 @@
 #include "copy.cuh"
 #include "ef.cuh"
 #include "grad.cuh"
+#include "launch.cuh"
 #include "persistent.cuh"
 #include "wait_selftest.cuh"
 #include "plus.cuh"
@@ -24,46 +25,17 @@
 
 using namespace ef21;
 
-#define CU(call)                                         \
-    do {                                                 \
-        cudaError_t e__ = (call);                        \
-        if (e__ != cudaSuccess) return EF21_ERR_CUDA;    \
-    } while (0)
-#define EF(call)                                         \
-    do {                                                 \
-        ef21_status s__ = (call);                        \
-        if (s__ != EF21_OK) return s__;                  \
-    } while (0)
-
-
 namespace {
 
-constexpr size_t ALIGN = 256;
 // Launch-path iterations up to this dimension are replayed as a CUDA graph.  Wider ones are launched one by one: a graph per iteration is
 // a full stop between iterations, across which the gradient kernel could not fetch its first rows (20 x 300 x 5,001: 41.2 us an
 // iteration without the graph, 43.1 with it; three launches take the host about 7 us).  EF21+, seven launches, 20 iterations one by one / replayed:
 // 20 x 600 x 700 554 / 597, 4 x 60 x 3,000 494 / 527, 20 x 200 x 5,001 800 / 831; 4 x 50 x 600 398 / 389, 2 x 30 x 513 400 / 398.
 constexpr i64 GRAPH_MAX_D = 512;
-inline size_t align_up(size_t v) { return (v + ALIGN - 1) / ALIGN * ALIGN; }
-inline i64 ceil_div(i64 a, i64 b) { return (a + b - 1) / b; }
 
 // ---------------------------------------------------------------------------------------------
 // Workspace layouts
 // ---------------------------------------------------------------------------------------------
-
-// Kernel launch as a programmatic dependent of whatever precedes it in the stream (see pdl_wait), with clusters of C blocks.
-template <typename... Params, typename... Args>
-cudaError_t launch(void (*kern)(Params...), dim3 grid, unsigned block, size_t smem, cudaStream_t st, unsigned C, Args... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid; cfg.blockDim = dim3(block); cfg.dynamicSmemBytes = smem; cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = C; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr; cfg.numAttrs = C > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kern, static_cast<Params>(args)...);
-}
 
 // Opt-in of a kernel to more dynamic shared memory than the default 48 KB (and to clusters of more than eight blocks): an
 // attribute per device, set once.

@@ -1,0 +1,368 @@
+// libef21: C-ABI entry points of a language model's worker -- objectives with their gradients, and the embedding table (see include/ef21.h).
+#include <cmath>
+
+#include "balance.cuh"
+#include "embedding.cuh"
+#include "launch.cuh"
+#include "policy.cuh"
+#include "preference.cuh"
+#include "token_logprobs.cuh"
+
+using namespace ef21;
+
+namespace {
+
+constexpr i64 MOST = 0x7fffffffll;            // rows, columns and positions are counted in 31 bits, elements in 63
+constexpr int SMS = 148;
+
+cudaStream_t stream_of(void* s) { return reinterpret_cast<cudaStream_t>(s); }
+bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+int bytes_of(int32_t dtype) { return dtype == EF21_DTYPE_F32 ? 4 : 2; }
+bool valid_dtype(int32_t dtype) { return dtype >= EF21_DTYPE_F32 && dtype <= EF21_DTYPE_F16; }
+bool valid_index(int32_t t) { return t == EF21_INDEX_I32 || t == EF21_INDEX_I64; }
+unsigned grid_of(i64 items, i64 per, i64 most) {
+    const i64 n = ceil_div(items, per);
+    return (unsigned)(n < 1 ? 1 : n > most ? most : n);
+}
+
+// f with a null pointer of the element type.
+template <typename F>
+ef21_status by_dtype(int32_t dtype, F f) {
+    switch (dtype) {
+        case EF21_DTYPE_F32: return f(static_cast<float*>(nullptr));
+        case EF21_DTYPE_BF16: return f(static_cast<__nv_bfloat16*>(nullptr));
+        default: return f(static_cast<__half*>(nullptr));
+    }
+}
+template <typename P> struct Pointee;
+template <typename T> struct Pointee<T*> { typedef T type; };
+
+// Sections of a workspace, 256-byte aligned.
+struct Sections {
+    char* base;
+    size_t used = 0;
+    explicit Sections(void* p) : base(static_cast<char*>(p)) {}
+    template <typename T> T* take(size_t n) {
+        T* p = reinterpret_cast<T*>(base + used);
+        used += align_up(n * sizeof(T));
+        return p;
+    }
+};
+bool workspace_fits(const void* p, size_t have, size_t need) { return p != nullptr && have >= need && aligned(p, ALIGN); }
+
+// ---- token log-probabilities --------------------------------------------------------------------------------------------------------------
+
+bool valid_logits(int32_t dtype, i64 batch, i64 length, i64 vocab, int32_t index, float scale) {
+    return valid_dtype(dtype) && valid_index(index) && batch >= 0 && length >= 0 && vocab >= 1 && vocab <= MOST && batch <= MOST && length <= MOST &&
+           batch * length <= MOST && std::isfinite(scale) && scale > 0.f;
+}
+
+// Blocks that share a row: one where the rows fill the device, up to eight of at least 2,048 columns each where they do not.
+unsigned logprob_cluster(i64 rows, i64 vocab) {
+    unsigned C = 1;
+    while (C < 8 && rows * C * 2 <= SMS * 4 && vocab / (C * 2) >= 2048) C *= 2;
+    return C;
+}
+
+// ---- policy loss: which kernel ------------------------------------------------------------------------------------------------------------
+
+struct PolicyWork { int* tokens; i64* counted; PolicySums* partial; };
+size_t policy_layout(void* p, i64 rows, PolicyWork& w) {
+    Sections s(p);
+    w.tokens = s.take<int>((size_t)rows);
+    w.counted = s.take<i64>(PO_MAX_BLOCKS);
+    w.partial = s.take<PolicySums>(PO_MAX_BLOCKS);
+    return s.used;
+}
+bool valid_rows(i64 rows, i64 length) { return rows >= 0 && length >= 0 && rows <= MOST && length <= MOST; }
+
+struct BalanceBuffers { BalanceWork* work; double* part; float* partial; };
+size_t balance_layout(void* p, i64 rows, i64 experts, BalanceBuffers& w) {
+    Sections s(p);
+    (void)rows;
+    w.work = s.take<BalanceWork>(1);
+    w.part = s.take<double>((size_t)ceil_div(experts, BL_FINISH_COLUMNS));
+    w.partial = s.take<float>((size_t)BL_MAX_BLOCKS * (size_t)experts);
+    return s.used;
+}
+
+// ---- embedding ----------------------------------------------------------------------------------------------------------------------------
+
+struct RadixPlan { int passes, bits; i64 tiles; };
+RadixPlan radix_plan(i64 count, i64 vocab) {
+    int need = 1;
+    while (need < 31 && (vocab >> need) != 0) ++need;                 // the key `vocab` itself is there too
+    RadixPlan p;
+    p.passes = (need + RX_MAX_BITS - 1) / RX_MAX_BITS;
+    p.bits = (need + p.passes - 1) / p.passes;
+    p.tiles = ceil_div(count, RX_TILE);
+    return p;
+}
+struct EmbeddingWork { int2 *runs, *sorted, *other; int *counts, *totals; float* partial; };
+size_t embedding_layout(void* p, i64 count, i64 vocab, i64 dim, EmbeddingWork& w) {
+    Sections s(p);
+    w.runs = s.take<int2>((size_t)vocab);
+    w.sorted = s.take<int2>((size_t)count);
+    w.other = nullptr; w.counts = w.totals = nullptr;
+    if (count > ED_RANK_TOKENS) {
+        w.other = s.take<int2>((size_t)count);
+        w.counts = s.take<int>((size_t)radix_plan(count, vocab).tiles << RX_MAX_BITS);
+        w.totals = s.take<int>(1 << RX_MAX_BITS);
+    }
+    w.partial = s.take<float>((size_t)ceil_div(count, ED_CHUNK) * 2 * (size_t)dim);
+    return s.used;
+}
+bool valid_table(i64 count, i64 vocab, i64 dim) {
+    return count >= 0 && count <= MOST - RX_TILE && vocab >= 1 && vocab < MOST && dim >= 1 && dim <= MOST;
+}
+
+// Sorted positions and the runs of all tokens.
+ef21_status enqueue_sort(cudaStream_t st, const void* tokens, int wide, i64 count, i64 vocab, i64 padding, const EmbeddingWork& w) {
+    CU(launch(embedding_clear_kernel, grid_of(vocab, ED_THREADS * 4, SMS * 8), ED_THREADS, 0, st, 1, w.runs, vocab));
+    if (count <= ED_RANK_TOKENS) {
+        CU(launch(embedding_rank_kernel, grid_of(count, ED_RANK_THREADS / 32, SMS * 4), ED_RANK_THREADS, (size_t)count * sizeof(int), st, 1, tokens, wide, (int)count, vocab, padding,
+                  w.sorted, w.runs));
+        return EF21_OK;
+    }
+    const RadixPlan p = radix_plan(count, vocab);
+    const int2* source = nullptr;
+    for (int k = 0; k < p.passes; ++k) {
+        int2* target = (p.passes - k) % 2 ? w.sorted : w.other;       // the last pass ends in `sorted`
+        CU(launch(radix_count_kernel, (unsigned)p.tiles, RX_THREADS, 0, st, 1, source, tokens, wide, count, vocab, padding, k * p.bits, p.bits, w.counts));
+        CU(launch(radix_places_kernel, (unsigned)ceil_div(1 << p.bits, 32), RX_THREADS, 0, st, 1, w.counts, w.totals, p.tiles, 1 << p.bits));
+        CU(launch(radix_move_kernel, (unsigned)p.tiles, RX_THREADS, 0, st, 1, source, tokens, wide, count, vocab, padding, k * p.bits, p.bits, w.counts, w.totals, target));
+        source = target;
+    }
+    CU(launch(embedding_runs_kernel, (unsigned)ceil_div(count, ED_THREADS), ED_THREADS, 0, st, 1, w.sorted, w.runs, count, vocab));
+    return EF21_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+ef21_status ef21_token_logprobs(const void* logits_dev, int32_t dtype, int64_t batch, int64_t length, int64_t vocab, int64_t batch_stride, int64_t row_stride,
+                                const void* targets_dev, int32_t index_type, int64_t targets_batch_stride, float scale, int64_t ignore,
+                                float* logps_out_dev, float* lse_out_dev, void* cuda_stream) {
+    if (!valid_logits(dtype, batch, length, vocab, index_type, scale)) return EF21_ERR_INVALID_ARG;
+    const i64 rows = batch * length;
+    if (rows == 0) return EF21_OK;
+    if (!logits_dev || !targets_dev || !logps_out_dev || !lse_out_dev || !aligned(logits_dev, bytes_of(dtype))) return EF21_ERR_INVALID_ARG;
+    const LogprobShape s{length, vocab, batch_stride, row_stride, targets_batch_stride, ignore, index_type, scale};
+    return by_dtype(dtype, [&](auto* type) -> ef21_status {
+        typedef typename Pointee<decltype(type)>::type T;
+        const T* logits = static_cast<const T*>(logits_dev);
+        cudaStream_t st = stream_of(cuda_stream);
+        if (vocab <= LP_WARP_VOCAB) {
+            CU(launch(logprobs_warp_kernel<T>, (unsigned)ceil_div(rows, LP_THREADS / 32), LP_THREADS, 0, st, 1, logits, targets_dev, logps_out_dev, lse_out_dev, s, rows));
+        } else {
+            const unsigned C = logprob_cluster(rows, vocab);
+            CU(launch(logprobs_block_kernel<T>, (unsigned)(rows * C), LP_THREADS, 0, st, C, logits, targets_dev, logps_out_dev, lse_out_dev, s, C));
+        }
+        return EF21_OK;
+    });
+}
+
+ef21_status ef21_token_logprobs_grad(const void* logits_dev, int32_t dtype, int64_t batch, int64_t length, int64_t vocab, int64_t batch_stride, int64_t row_stride,
+                                     const void* targets_dev, int32_t index_type, int64_t targets_batch_stride, const float* lse_dev, const float* grad_dev,
+                                     float scale, int64_t ignore, void* out_dev, int64_t out_batch_stride, int64_t out_row_stride, void* cuda_stream) {
+    if (!valid_logits(dtype, batch, length, vocab, index_type, scale)) return EF21_ERR_INVALID_ARG;
+    const i64 rows = batch * length;
+    if (rows == 0) return EF21_OK;
+    if (!logits_dev || !targets_dev || !lse_dev || !grad_dev || !out_dev || !aligned(logits_dev, bytes_of(dtype)) || !aligned(out_dev, bytes_of(dtype)))
+        return EF21_ERR_INVALID_ARG;
+    const LogprobShape s{length, vocab, batch_stride, row_stride, targets_batch_stride, ignore, index_type, scale};
+    return by_dtype(dtype, [&](auto* type) -> ef21_status {
+        typedef typename Pointee<decltype(type)>::type T;
+        const T* logits = static_cast<const T*>(logits_dev);
+        T* out = static_cast<T*>(out_dev);
+        cudaStream_t st = stream_of(cuda_stream);
+        if (vocab <= LP_WARP_VOCAB) {
+            CU(launch(logprobs_grad_warp_kernel<T>, (unsigned)ceil_div(rows, LP_THREADS / 32), LP_THREADS, 0, st, 1, logits, targets_dev, lse_dev, grad_dev, out, s, out_batch_stride,
+                      out_row_stride, rows));
+            return EF21_OK;
+        }
+        const i64 slab = (i64)LP_THREADS * Elem<T>::VEC * LP_UNROLL * 2, slabs = ceil_div(vocab, slab);
+        if (rows * slabs > MOST) return EF21_ERR_UNSUPPORTED;         // (more than 2^31 slabs of 16 KB or more: no device holds them)
+        CU(launch(logprobs_grad_block_kernel<T>, (unsigned)(rows * slabs), LP_THREADS, 0, st, 1, logits, targets_dev, lse_dev, grad_dev, out, s, out_batch_stride, out_row_stride,
+                  (unsigned)slabs, slab));
+        return EF21_OK;
+    });
+}
+
+size_t ef21_preference_loss_workspace_bytes(int64_t pairs, int64_t length) {
+    return pairs < 1 || pairs > MOST / 2 || length < 0 || length > MOST ? 0 : align_up(sizeof(double) * (size_t)grid_of(pairs, 1, SMS * 8));
+}
+
+ef21_status ef21_preference_loss(const void* logps_dev, const void* ref_dev, const uint8_t* mask_dev, int32_t dtype, int64_t pairs, int64_t length,
+                                 int64_t logps_stride, int64_t ref_stride, int64_t mask_stride, double beta, double smoothing, double norm,
+                                 float* loss_out_dev, float* rewards_out_dev, void* grad_out_dev, void* workspace_dev, size_t workspace_bytes, void* cuda_stream) {
+    const size_t need = ef21_preference_loss_workspace_bytes(pairs, length);
+    if (need == 0 || !valid_dtype(dtype) || !std::isfinite(beta) || !(smoothing >= 0.0 && smoothing <= 1.0) || !(norm > 0.0) || !std::isfinite(norm)) return EF21_ERR_INVALID_ARG;
+    if (!loss_out_dev || !rewards_out_dev || (length > 0 && (!logps_dev || !grad_out_dev))) return EF21_ERR_INVALID_ARG;
+    const size_t e = bytes_of(dtype);
+    if (!aligned(logps_dev, e) || !aligned(ref_dev, e) || !aligned(grad_out_dev, e)) return EF21_ERR_INVALID_ARG;
+    if (!workspace_fits(workspace_dev, workspace_bytes, need)) return EF21_ERR_WORKSPACE;
+    double* partial = static_cast<double*>(workspace_dev);
+    const unsigned blocks = grid_of(pairs, 1, SMS * 8);
+    cudaStream_t st = stream_of(cuda_stream);
+    return by_dtype(dtype, [&](auto* type) -> ef21_status {
+        typedef typename Pointee<decltype(type)>::type T;
+        constexpr int VEC = Elem<T>::VEC;
+        const T *logps = static_cast<const T*>(logps_dev), *ref = static_cast<const T*>(ref_dev);
+        T* grad = static_cast<T*>(grad_out_dev);
+        const PreferenceShape s{pairs, length, logps_stride, ref_stride, mask_stride, beta, smoothing, norm};
+        const bool vectors = aligned(logps, 16) && aligned(ref, 16) && aligned(grad, 16) && aligned(mask_dev, VEC) && (logps_stride - length) % VEC == 0 &&
+                             (!ref || (ref_stride - length) % VEC == 0) && (!mask_dev || (mask_stride - length) % VEC == 0);
+        if (vectors) CU(launch(preference_kernel<T, true>, blocks, PF_THREADS, 0, st, 1, logps, ref, mask_dev, rewards_out_dev, grad, partial, s));
+        else CU(launch(preference_kernel<T, false>, blocks, PF_THREADS, 0, st, 1, logps, ref, mask_dev, rewards_out_dev, grad, partial, s));
+        CU(launch(preference_finish_kernel, 1, PF_THREADS, 0, st, 1, partial, loss_out_dev, (int)blocks, norm));
+        return EF21_OK;
+    });
+}
+
+size_t ef21_policy_loss_workspace_bytes(int64_t rows, int64_t length) {
+    PolicyWork w;
+    return valid_rows(rows, length) ? policy_layout(nullptr, rows, w) : 0;
+}
+
+ef21_status ef21_policy_loss(const void* logps_dev, const void* old_dev, const void* ref_dev, const void* advantages_dev, const uint8_t* mask_dev, int32_t dtype,
+                             int64_t rows, int64_t length, int64_t logps_stride, int64_t old_stride, int64_t ref_stride, int64_t advantages_stride, int64_t mask_stride,
+                             int32_t advantages_per_token, double clip_low, double clip_high, double kl_weight, int32_t reduction, double norm,
+                             float* terms_out_dev, void* grad_out_dev, void* workspace_dev, size_t workspace_bytes, void* cuda_stream) {
+    const size_t need = ef21_policy_loss_workspace_bytes(rows, length);
+    if (need == 0 || !valid_dtype(dtype) || !(clip_low >= 0.0 && clip_low < 1.0) || !(clip_high >= 0.0) || !std::isfinite(clip_high) || !std::isfinite(kl_weight) ||
+        (reduction != EF21_REDUCE_TOKENS && reduction != EF21_REDUCE_SEQUENCES) || !(norm >= 0.0) || !std::isfinite(norm) || (!ref_dev && kl_weight != 0.0))
+        return EF21_ERR_INVALID_ARG;
+    if (!terms_out_dev || (rows * length > 0 && (!logps_dev || !old_dev || !advantages_dev || !grad_out_dev))) return EF21_ERR_INVALID_ARG;
+    const size_t e = bytes_of(dtype);
+    if (!aligned(logps_dev, e) || !aligned(old_dev, e) || !aligned(ref_dev, e) || !aligned(advantages_dev, e) || !aligned(grad_out_dev, e)) return EF21_ERR_INVALID_ARG;
+    if (!workspace_fits(workspace_dev, workspace_bytes, need)) return EF21_ERR_WORKSPACE;
+    PolicyWork w;
+    policy_layout(workspace_dev, rows, w);
+    cudaStream_t st = stream_of(cuda_stream);
+    const bool by_sequence = reduction == EF21_REDUCE_SEQUENCES, count = mask_dev && (norm == 0.0 || by_sequence);
+    const unsigned count_blocks = grid_of(rows, PO_THREADS / 32, PO_MAX_BLOCKS);
+    if (count) CU(launch(policy_count_kernel, count_blocks, PO_THREADS, 0, st, 1, mask_dev, w.tokens, w.counted, rows, length, mask_stride, (int)by_sequence));
+    return by_dtype(dtype, [&](auto* type) -> ef21_status {
+        typedef typename Pointee<decltype(type)>::type T;
+        constexpr int VEC = Elem<T>::VEC;
+        const T *logps = static_cast<const T*>(logps_dev), *old = static_cast<const T*>(old_dev), *ref = static_cast<const T*>(ref_dev), *adv = static_cast<const T*>(advantages_dev);
+        T* grad = static_cast<T*>(grad_out_dev);
+        const PolicyShape s{rows, length, logps_stride, old_stride, ref_stride, mask_stride, advantages_stride, advantages_per_token, by_sequence,
+                            std::log1p(-clip_low), std::log1p(clip_high), (float)(1.0 - clip_low), (float)(1.0 + clip_high), (float)kl_weight, norm, (int)count_blocks};
+        auto whole = [&](const void* p, i64 stride) { return aligned(p, 16) && (!p || rows <= 1 || stride == length); };
+        const bool flat = whole(logps, logps_stride) && whole(old, old_stride) && whole(ref, ref_stride) && (!advantages_per_token || whole(adv, advantages_stride)) &&
+                          aligned(grad, 16) && aligned(mask_dev, VEC) && (!mask_dev || rows <= 1 || mask_stride == length);
+        const i64 all = rows * length;
+        const unsigned blocks = grid_of(all, (i64)PO_THREADS * (flat ? VEC : 1), PO_MAX_BLOCKS);
+        const int* tokens = count ? w.tokens : nullptr;
+        const i64* counted = count ? w.counted : nullptr;
+        if (flat) CU(launch(policy_kernel<T, true>, blocks, PO_THREADS, 0, st, 1, logps, old, ref, adv, mask_dev, tokens, counted, grad, w.partial, s));
+        else CU(launch(policy_kernel<T, false>, blocks, PO_THREADS, 0, st, 1, logps, old, ref, adv, mask_dev, tokens, counted, grad, w.partial, s));
+        CU(launch(policy_finish_kernel, 1, PO_THREADS, 0, st, 1, w.partial, terms_out_dev, (int)blocks, kl_weight));
+        return EF21_OK;
+    });
+}
+
+size_t ef21_balance_loss_workspace_bytes(int64_t rows, int64_t experts) {
+    BalanceBuffers w;
+    return rows < 0 || rows > MOST || experts < 1 || experts > BL_MAX_EXPERTS ? 0 : balance_layout(nullptr, rows, experts, w);
+}
+
+ef21_status ef21_balance_loss(const void* logits_dev, int32_t dtype, int64_t rows, int64_t experts, int64_t logits_stride, const void* choices_dev, int32_t index_type, int64_t chosen,
+                              int64_t choices_stride, const uint8_t* mask_dev, double weight, float* loss_out_dev, int32_t* counts_out_dev, float* probs_out_dev, void* grad_out_dev,
+                              void* workspace_dev, size_t workspace_bytes, void* cuda_stream) {
+    const size_t need = ef21_balance_loss_workspace_bytes(rows, experts);
+    if (need == 0 || !valid_dtype(dtype) || !valid_index(index_type) || chosen < 1 || chosen > experts || rows * chosen > MOST || !std::isfinite(weight)) return EF21_ERR_INVALID_ARG;
+    if (!loss_out_dev || !counts_out_dev || !probs_out_dev || (rows > 0 && (!logits_dev || !choices_dev || !grad_out_dev))) return EF21_ERR_INVALID_ARG;
+    if (!aligned(logits_dev, bytes_of(dtype)) || !aligned(grad_out_dev, bytes_of(dtype))) return EF21_ERR_INVALID_ARG;
+    if (!workspace_fits(workspace_dev, workspace_bytes, need)) return EF21_ERR_WORKSPACE;
+    BalanceBuffers w;
+    balance_layout(workspace_dev, rows, experts, w);
+    cudaStream_t st = stream_of(cuda_stream);
+    const BalanceShape s{rows, (int)experts, (int)chosen, index_type, logits_stride, choices_stride, weight};
+    CU(launch(balance_clear_kernel, 1, BL_THREADS, 0, st, 1, counts_out_dev, w.work, (int)experts));
+    CU(launch(balance_count_kernel, grid_of(rows * chosen, BL_THREADS * 4, SMS * 2), BL_THREADS, 0, st, 1, choices_dev, mask_dev, counts_out_dev, w.work, s));
+    int lanes = 1;
+    while (lanes < 32 && lanes < experts) lanes *= 2;
+    const unsigned blocks = grid_of(rows, BL_THREADS / lanes, BL_MAX_BLOCKS);
+    EF(by_dtype(dtype, [&](auto* type) -> ef21_status {
+        typedef typename Pointee<decltype(type)>::type T;
+        const T* logits = static_cast<const T*>(logits_dev);
+        T* grad = static_cast<T*>(grad_out_dev);
+        auto run = [&](auto kernel) -> ef21_status {
+            CU(launch(kernel, blocks, BL_THREADS, 0, st, 1, logits, mask_dev, counts_out_dev, w.work, grad, w.partial, s, lanes));
+            return EF21_OK;
+        };
+        if (experts <= 32) return run(balance_kernel<T, 1>);
+        if (experts <= 64) return run(balance_kernel<T, 2>);
+        if (experts <= 128) return run(balance_kernel<T, 4>);
+        if (experts <= 256) return run(balance_kernel<T, 8>);
+        if (experts <= 512) return run(balance_kernel<T, 16>);
+        return run(balance_kernel<T, 32>);
+    }));
+    CU(launch(balance_finish_kernel, (unsigned)ceil_div(experts, BL_FINISH_COLUMNS), BL_FINISH_COLUMNS * BL_FINISH_GROUPS, 0, st, 1, w.partial, counts_out_dev, w.work, w.part,
+              probs_out_dev, loss_out_dev, (int)blocks, (int)experts, (int)chosen, weight));
+    return EF21_OK;
+}
+
+ef21_status ef21_embedding(const void* weight_dev, int32_t dtype, int64_t vocab, int64_t dim, int64_t weight_stride, const void* tokens_dev, int32_t index_type, int64_t count, float scale,
+                           void* out_dev, void* cuda_stream) {
+    if (!valid_dtype(dtype) || !valid_index(index_type) || !valid_table(count, vocab, dim) || !std::isfinite(scale)) return EF21_ERR_INVALID_ARG;
+    if (count == 0) return EF21_OK;
+    if (!weight_dev || !tokens_dev || !out_dev || !aligned(weight_dev, bytes_of(dtype)) || !aligned(out_dev, bytes_of(dtype))) return EF21_ERR_INVALID_ARG;
+    return by_dtype(dtype, [&](auto* type) -> ef21_status {
+        typedef typename Pointee<decltype(type)>::type T;
+        constexpr int VEC = Elem<T>::VEC;
+        const T* weight = static_cast<const T*>(weight_dev);
+        T* out = static_cast<T*>(out_dev);
+        cudaStream_t st = stream_of(cuda_stream);
+        if (aligned(weight, 16) && aligned(out, 16) && dim % VEC == 0 && weight_stride % VEC == 0)
+            CU(launch(embedding_kernel<T, true>, grid_of(count * (dim / VEC), ED_THREADS, MOST), ED_THREADS, 0, st, 1, weight, tokens_dev, out, count, vocab, dim, weight_stride, index_type, scale));
+        else
+            CU(launch(embedding_kernel<T, false>, grid_of(count * dim, ED_THREADS, MOST), ED_THREADS, 0, st, 1, weight, tokens_dev, out, count, vocab, dim, weight_stride, index_type, scale));
+        return EF21_OK;
+    });
+}
+
+size_t ef21_embedding_grad_workspace_bytes(int64_t count, int64_t vocab, int64_t dim) {
+    EmbeddingWork w;
+    return valid_table(count, vocab, dim) ? embedding_layout(nullptr, count, vocab, dim, w) : 0;
+}
+
+ef21_status ef21_embedding_grad(const void* grad_dev, int32_t dtype, int64_t count, int64_t dim, int64_t grad_stride, const void* tokens_dev, int32_t index_type, int64_t vocab,
+                                int64_t padding, float scale, void* out_dev, int32_t out_dtype, int64_t out_stride, int32_t accumulate, void* workspace_dev, size_t workspace_bytes,
+                                void* cuda_stream) {
+    const size_t need = ef21_embedding_grad_workspace_bytes(count, vocab, dim);
+    if (need == 0 || !valid_dtype(dtype) || (out_dtype != dtype && out_dtype != EF21_DTYPE_F32) || !valid_index(index_type) || !std::isfinite(scale) || !out_dev ||
+        (count > 0 && (!grad_dev || !tokens_dev)) || !aligned(grad_dev, bytes_of(dtype)) || !aligned(out_dev, bytes_of(out_dtype)))
+        return EF21_ERR_INVALID_ARG;
+    if (!workspace_fits(workspace_dev, workspace_bytes, need)) return EF21_ERR_WORKSPACE;
+    EmbeddingWork w;
+    embedding_layout(workspace_dev, count, vocab, dim, w);
+    cudaStream_t st = stream_of(cuda_stream);
+    EF(enqueue_sort(st, tokens_dev, index_type, count, vocab, padding, w));
+    return by_dtype(dtype, [&](auto* type) -> ef21_status {
+        typedef typename Pointee<decltype(type)>::type T;
+        const T* grad = static_cast<const T*>(grad_dev);
+        const bool vectors = aligned(grad, 16) && dim % Elem<T>::VEC == 0 && grad_stride % Elem<T>::VEC == 0;
+        if (count > ED_CHUNK) {
+            const unsigned chunks = (unsigned)ceil_div(count, ED_CHUNK);
+            if (vectors) CU(launch(embedding_long_kernel<T, true>, chunks, ED_THREADS, 0, st, 1, grad, w.sorted, w.runs, w.partial, count, vocab, dim, grad_stride));
+            else CU(launch(embedding_long_kernel<T, false>, chunks, ED_THREADS, 0, st, 1, grad, w.sorted, w.runs, w.partial, count, vocab, dim, grad_stride));
+        }
+        auto rows = [&](auto kernel, auto* out) -> ef21_status {
+            CU(launch(kernel, (unsigned)vocab, ED_THREADS, 0, st, 1, grad, w.sorted, w.runs, w.partial, out, dim, grad_stride, out_stride, scale, accumulate));
+            return EF21_OK;
+        };
+        if (out_dtype == EF21_DTYPE_F32) {
+            float* out = static_cast<float*>(out_dev);
+            return vectors ? rows(embedding_rows_kernel<T, float, true>, out) : rows(embedding_rows_kernel<T, float, false>, out);
+        }
+        T* out = static_cast<T*>(out_dev);
+        return vectors ? rows(embedding_rows_kernel<T, T, true>, out) : rows(embedding_rows_kernel<T, T, false>, out);
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,247 @@
+// Log-probabilities of given tokens from rows of logits, and the logits' gradient.
+//
+//   lse_r  = log sum_j exp(s x_rj)          logp_r = s x_r,t(r) - lse_r
+//   dx_rj  = s g_r (1[j = t(r)] - exp(s x_rj - lse_r))
+//
+// Both directions read every logit once; the forward pass carries the running maximum m and the sum of 2^((x - m) c), c = s log2 e.  The maximum
+// is subtracted before anything is multiplied: a row that a mask of the type's lowest value leaves nothing of must not overflow.
+#pragma once
+#include "element.cuh"
+
+namespace ef21 {
+
+struct LogprobShape {
+    i64 length, vocab;                      // rows per batch entry, columns
+    i64 batch_stride, row_stride;           // logits, in elements
+    i64 target_stride;                      // targets per batch entry
+    i64 ignore;
+    int wide;                               // 64-bit targets
+    float scale;
+};
+
+constexpr int LP_THREADS = 256;
+constexpr int LP_UNROLL = 4;                // vectors of 16 bytes per thread in flight
+constexpr i64 LP_WARP_VOCAB = 2048;         // rows up to this length belong to one warp
+
+// Maximum and sum of 2^((x - m) c) over what a thread has seen; m = -inf: nothing but -inf so far.
+struct Running { float m = -INFINITY, s = 0.f; };
+
+__device__ __forceinline__ Running merge(Running a, Running b, float c) {
+    Running r;
+    r.m = fmaxf(a.m, b.m);
+    const float base = r.m == -INFINITY ? 0.f : r.m;
+    r.s = a.s * exp2_fast((a.m - base) * c) + b.s * exp2_fast((b.m - base) * c);      // (a NaN stays one; +inf makes one: inf - inf)
+    return r;
+}
+
+__device__ __forceinline__ Running warp_merge(Running r, float c) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        Running other;
+        other.m = __shfl_xor_sync(0xffffffffu, r.m, o);
+        other.s = __shfl_xor_sync(0xffffffffu, r.s, o);
+        r = merge(r, other, c);
+    }
+    return r;
+}
+
+template <typename T>
+__device__ __forceinline__ void run_one(const T* x, float c, Running& r) {
+    const float v = Elem<T>::get(*x);
+    Running one;
+    if (v == v) { one.m = v; one.s = v == -INFINITY ? 0.f : 1.f; } else one.s = NAN;
+    r = merge(r, one, c);
+}
+
+// `count` elements from x on, shared by `threads` threads.
+template <typename T>
+__device__ __forceinline__ Running run_span(const T* x, i64 count, float c, int tid, int threads) {
+    constexpr int VEC = Elem<T>::VEC;
+    Running r;
+    const i64 head = min((i64)row_head(x), count), vectors = (count - head) / VEC, tail = count - head - vectors * VEC;
+    if (tid < head) run_one(x + tid, c, r);
+    if (tid < tail) run_one(x + count - tail + tid, c, r);
+    const T* body = x + head;
+    for (i64 v = tid; v < vectors; v += (i64)threads * LP_UNROLL) {
+        uint4 u[LP_UNROLL];
+#pragma unroll
+        for (int k = 0; k < LP_UNROLL; ++k) {
+            const i64 at = v + (i64)k * threads;
+            u[k] = at < vectors ? load_once(body + at * VEC) : make_uint4(Elem<T>::NEG_INF, Elem<T>::NEG_INF, Elem<T>::NEG_INF, Elem<T>::NEG_INF);
+        }
+        float top = Elem<T>::top(u[0]);
+#pragma unroll
+        for (int k = 1; k < LP_UNROLL; ++k) top = fmaxf(top, Elem<T>::top(u[k]));
+        const float m = fmaxf(r.m, top), base = m == -INFINITY ? 0.f : m;
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < LP_UNROLL; ++k) {
+            float f[VEC];
+            Elem<T>::unpack(u[k], f);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum += exp2_fast((f[e] - base) * c);
+        }
+        r.s = r.s * exp2_fast((r.m - base) * c) + sum;
+        r.m = m;
+    }
+    return r;
+}
+
+__device__ __forceinline__ void write_logprob(Running r, float xt, bool inside, float scale, float c, float* logp, float* lse) {
+    const float l = log2f(r.s);
+    if (!inside) { *logp = NAN; *lse = NAN; }
+    else if (r.s == 0.f) { *logp = -INFINITY; *lse = -INFINITY; }          // no logit but -inf: no distribution
+    else { *logp = fmaf(xt - r.m, c, -l) * LN2; *lse = fmaf(r.m, scale, l * LN2); }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(LP_THREADS) logprobs_warp_kernel(const T* logits, const void* targets, float* logps, float* lse, LogprobShape s, i64 rows) {
+    pdl_wait(logits, targets, logps, lse);
+    pdl_trigger();
+    const int lane = threadIdx.x & 31;
+    const i64 row = (i64)blockIdx.x * (LP_THREADS / 32) + (threadIdx.x >> 5);
+    if (row >= rows) return;
+    const i64 b = row / s.length, t = row - b * s.length;
+    const i64 target = index_at(targets, s.wide, b * s.target_stride + t);
+    if (target == s.ignore) {
+        if (lane == 0) { logps[row] = 0.f; lse[row] = 0.f; }
+        return;
+    }
+    const T* x = logits + b * s.batch_stride + t * s.row_stride;
+    const bool inside = target >= 0 && target < s.vocab;
+    const float xt = inside ? Elem<T>::get(x[target]) : 0.f, c = s.scale * LOG2E;
+    const Running r = warp_merge(run_span(x, s.vocab, c, lane, 32), c);
+    if (lane == 0) write_logprob(r, xt, inside, s.scale, c, logps + row, lse + row);
+}
+
+// One cluster per row, its blocks an equal share of the columns each.
+template <typename T>
+__global__ void __launch_bounds__(LP_THREADS) logprobs_block_kernel(const T* logits, const void* targets, float* logps, float* lse, LogprobShape s, unsigned C) {
+    pdl_wait(logits, targets, logps, lse);
+    pdl_trigger();
+    __shared__ Running part[LP_THREADS / 32], whole;
+    const int tid = threadIdx.x;
+    const i64 row = blockIdx.x / C;
+    const unsigned rank = blockIdx.x - (unsigned)row * C;
+    const i64 b = row / s.length, t = row - b * s.length;
+    const i64 target = index_at(targets, s.wide, b * s.target_stride + t);
+    if (target == s.ignore) {                                  // (all blocks of the cluster alike)
+        if (tid == 0 && rank == 0) { logps[row] = 0.f; lse[row] = 0.f; }
+        return;
+    }
+    const T* x = logits + b * s.batch_stride + t * s.row_stride;
+    const bool inside = target >= 0 && target < s.vocab;
+    const float c = s.scale * LOG2E;
+    const float xt = inside && tid == 0 && rank == 0 ? Elem<T>::get(x[target]) : 0.f;
+    const i64 share = (s.vocab + C - 1) / C, begin = min(rank * share, s.vocab), end = min(begin + share, s.vocab);
+    Running r = warp_merge(run_span(x + begin, end - begin, c, tid, LP_THREADS), c);
+    if ((tid & 31) == 0) part[tid >> 5] = r;
+    __syncthreads();
+    if (tid < 32) {
+        Running w;
+        if (tid < LP_THREADS / 32) w = part[tid];
+        r = warp_merge(w, c);
+    }
+    if (C > 1) {
+        if (tid == 0) whole = r;
+        asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+        if (rank == 0 && tid < 32) {
+            Running w;
+            if (tid < (int)C) {
+                unsigned at = (unsigned)__cvta_generic_to_shared(&whole), remote;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(at), "r"(tid));
+                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(w.m), "=f"(w.s) : "r"(remote) : "memory");
+            }
+            r = warp_merge(w, c);
+        }
+        asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");      // nobody leaves while it is read
+    }
+    if (tid == 0 && rank == 0) write_logprob(r, xt, inside, s.scale, c, logps + row, lse + row);
+}
+
+// What the gradient of one row needs: dx_j = a 1[j = target] - a exp(scale x_j - lse).
+struct RowGrad {
+    float a, scale, lse;
+    i64 target;
+    bool zero;
+};
+
+__device__ __forceinline__ RowGrad row_grad(const void* targets, const float* lse, const float* grad, const LogprobShape& s, i64 row, i64 b, i64 t) {
+    RowGrad r;
+    r.target = index_at(targets, s.wide, b * s.target_stride + t);
+    const float l = lse[row];
+    r.a = grad[row] * s.scale;
+    r.scale = s.scale;
+    r.zero = r.target == s.ignore || grad[row] == 0.f || l == -INFINITY;
+    r.lse = r.target >= 0 && r.target < s.vocab ? l : NAN;
+    return r;
+}
+
+// Columns [begin, end) of one row.
+template <typename T>
+__device__ __forceinline__ void grad_span(const T* x, T* out, i64 begin, i64 end, const RowGrad& r, int tid, int threads) {
+    constexpr int VEC = Elem<T>::VEC;
+    auto value = [&](float f, i64 j) {
+        const float p = r.a * exp2_fast(fmaf(f, r.scale, -r.lse) * LOG2E);
+        return j == r.target ? r.a - p : -p;
+    };
+    auto one = [&](i64 j) { out[j] = Elem<T>::put(r.zero ? 0.f : value(Elem<T>::get(x[j]), j)); };
+    if (row_head(x + begin) != row_head(out + begin)) {       // rows of different alignment: element by element
+        for (i64 j = begin + tid; j < end; j += threads) one(j);
+        return;
+    }
+    const i64 head = min((i64)row_head(x + begin), end - begin), vectors = (end - begin - head) / VEC, tail = end - begin - head - vectors * VEC;
+    if (tid < head) one(begin + tid);
+    if (tid < tail) one(end - tail + tid);
+    const i64 body = begin + head;
+    for (i64 v = tid; v < vectors; v += (i64)threads * LP_UNROLL) {
+        uint4 u[LP_UNROLL];
+#pragma unroll
+        for (int k = 0; k < LP_UNROLL; ++k) {
+            const i64 at = v + (i64)k * threads;
+            if (at < vectors && !r.zero) u[k] = load_once(x + body + at * VEC);
+        }
+#pragma unroll
+        for (int k = 0; k < LP_UNROLL; ++k) {
+            const i64 at = v + (i64)k * threads, j = body + at * VEC;
+            if (at >= vectors) break;
+            if (r.zero) { store_vec(out + j, make_uint4(0u, 0u, 0u, 0u)); continue; }
+            float f[VEC];
+            Elem<T>::unpack(u[k], f);
+            const bool named = r.target >= j && r.target < j + VEC;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) f[e] = -r.a * exp2_fast(fmaf(f[e], r.scale, -r.lse) * LOG2E);
+            if (named) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) if (j + e == r.target) f[e] += r.a;
+            }
+            store_vec(out + j, Elem<T>::pack(f));
+        }
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(LP_THREADS) logprobs_grad_warp_kernel(const T* logits, const void* targets, const float* lse, const float* grad, T* out,
+                                                                        LogprobShape s, i64 out_batch_stride, i64 out_row_stride, i64 rows) {
+    pdl_wait(logits, targets, lse, grad, out);
+    pdl_trigger();
+    const i64 row = (i64)blockIdx.x * (LP_THREADS / 32) + (threadIdx.x >> 5);
+    if (row >= rows) return;
+    const i64 b = row / s.length, t = row - b * s.length;
+    const RowGrad r = row_grad(targets, lse, grad, s, row, b, t);
+    grad_span(logits + b * s.batch_stride + t * s.row_stride, out + b * out_batch_stride + t * out_row_stride, 0, s.vocab, r, threadIdx.x & 31, 32);
+}
+
+// One block per slab of a row's columns.
+template <typename T>
+__global__ void __launch_bounds__(LP_THREADS) logprobs_grad_block_kernel(const T* logits, const void* targets, const float* lse, const float* grad, T* out,
+                                                                         LogprobShape s, i64 out_batch_stride, i64 out_row_stride, unsigned slabs, i64 slab) {
+    pdl_wait(logits, targets, lse, grad, out);
+    pdl_trigger();
+    const i64 row = blockIdx.x / slabs, at = (i64)(blockIdx.x - (unsigned)row * slabs) * slab;
+    const i64 b = row / s.length, t = row - b * s.length;
+    const RowGrad r = row_grad(targets, lse, grad, s, row, b, t);
+    grad_span(logits + b * s.batch_stride + t * s.row_stride, out + b * out_batch_stride + t * out_row_stride, at, min(at + slab, s.vocab), r, threadIdx.x, LP_THREADS);
+}
+
+}  // namespace ef21
