@@ -3,9 +3,9 @@
 //
 //   out_t = s W[tok_t]          dW_v = s sum_{t: tok_t = v} g_t
 //
-// The gradient is no scatter (float atomics add in any order): positions are sorted by token (stable), then every row of the table is formed
-// by one block from its run of positions and written once, zeros where no token names it.  A run of more than ED_CHUNK positions is
-// added up ED_CHUNK sorted positions at a time by blocks of their own, whose sums its row adds in order.
+// The gradient is no scatter (float atomics add in any order): positions are sorted by token (stable); then every row of the table that
+// has at most ED_CHUNK positions is formed by the lanes of one team and written once, zeros where no token names it, while other blocks of the same
+// launch add up the longer runs ED_CHUNK sorted positions at a time; a last launch joins these sums, in order.
 //
 // Sorting: up to ED_RANK_TOKENS tokens by counting, for every token, those in front of it -- one launch; more by a radix sort, digits of up to nine bits.
 #pragma once
@@ -14,37 +14,52 @@
 namespace ef21 {
 
 constexpr int ED_THREADS = 256;
-constexpr int ED_CHUNK = 32;
+constexpr int ED_CHUNK = 32;                // sorted positions that one team adds up
+constexpr int ED_VECS = 2;                  // vectors per lane and row
+constexpr int ED_ROW_VECS = 4;
+constexpr int ED_SHARES = ED_THREADS / 32;
 constexpr int ED_RANK_TOKENS = 8192;
 constexpr int ED_RANK_THREADS = 256;
 constexpr int RX_THREADS = 1024, RX_ITEMS = 4, RX_TILE = RX_THREADS * RX_ITEMS, RX_MAX_BITS = 9, RX_WARPS = RX_THREADS / 32;
 
 // ---- lookup -------------------------------------------------------------------------------------------------------------------------------
 
-// VECTORS: rows are whole numbers of 16 bytes and aligned.  One thread per 16 bytes (or element) of the output.
+// A warp takes ED_ROW_VECS times 32 vectors (VECTORS: 16 bytes, rows are whole numbers of them and aligned; else elements) of one row.
 template <typename T, bool VECTORS>
-__global__ void __launch_bounds__(ED_THREADS) embedding_kernel(const T* weight, const void* tokens, T* out, i64 count, i64 vocab, i64 dim, i64 stride, int wide, float scale) {
+__global__ void __launch_bounds__(ED_THREADS) embedding_kernel(const T* weight, const void* tokens, T* out, i64 items, int slabs, i64 vocab, i64 dim, i64 stride, int wide, float scale) {
     pdl_wait(weight, tokens, out);
     pdl_trigger();
     constexpr int VEC = VECTORS ? Elem<T>::VEC : 1;
-    const i64 per = dim / VEC, all = count * per;
-    for (i64 i = (i64)blockIdx.x * ED_THREADS + threadIdx.x; i < all; i += (i64)gridDim.x * ED_THREADS) {
-        const i64 t = i / per, j = (i - t * per) * VEC;
-        const i64 v = index_at(tokens, wide, t);
-        const bool in = v >= 0 && v < vocab;
-        if (VECTORS) {
-            float f[Elem<T>::VEC];
-            Elem<T>::unpack(in ? *reinterpret_cast<const uint4*>(weight + v * stride + j) : make_uint4(0u, 0u, 0u, 0u), f);
+    const i64 item = (i64)blockIdx.x * (ED_THREADS / 32) + (threadIdx.x >> 5);
+    if (item >= items) return;
+    const i64 t = slabs == 1 ? item : item / slabs;
+    const i64 first = (item - t * slabs) * (32 * ED_ROW_VECS * VEC) + (threadIdx.x & 31) * VEC;
+    const i64 v = index_at(tokens, wide, t);
+    const bool in = v >= 0 && v < vocab;
+    const T* row = weight + (in ? v : 0) * stride;
+    T* o = out + t * dim;
+    if (VECTORS) {
+        uint4 u[ED_ROW_VECS];
 #pragma unroll
-            for (int e = 0; e < Elem<T>::VEC; ++e) f[e] *= scale;
-            if (!in) {
-#pragma unroll
-                for (int e = 0; e < Elem<T>::VEC; ++e) f[e] = 0.f;
-            }
-            store_vec(out + t * dim + j, Elem<T>::pack(f));
-        } else {
-            out[t * dim + j] = Elem<T>::put(in ? Elem<T>::get(weight[v * stride + j]) * scale : 0.f);
+        for (int k = 0; k < ED_ROW_VECS; ++k) {
+            const i64 j = first + k * 32 * VEC;
+            u[k] = in && j < dim ? *reinterpret_cast<const uint4*>(row + j) : make_uint4(0u, 0u, 0u, 0u);
         }
+#pragma unroll
+        for (int k = 0; k < ED_ROW_VECS; ++k) {
+            const i64 j = first + k * 32 * VEC;
+            float f[Elem<T>::VEC];
+            Elem<T>::unpack(u[k], f);
+#pragma unroll
+            for (int e = 0; e < Elem<T>::VEC; ++e) f[e] = in ? f[e] * scale : 0.f;
+            if (j < dim) store_vec(o + j, Elem<T>::pack(f));
+        }
+    } else {
+        float f[ED_ROW_VECS];
+#pragma unroll
+        for (int k = 0; k < ED_ROW_VECS; ++k) f[k] = in && first + k * 32 < dim ? Elem<T>::get(row[first + k * 32]) : 0.f;
+#pragma unroll
+        for (int k = 0; k < ED_ROW_VECS; ++k) if (first + k * 32 < dim) o[first + k * 32] = Elem<T>::put(in ? f[k] * scale : 0.f);
     }
 }
 
@@ -54,13 +69,6 @@ __global__ void __launch_bounds__(ED_THREADS) embedding_kernel(const T* weight, 
 __device__ __forceinline__ int token_key(const void* tokens, int wide, i64 i, i64 vocab, i64 padding) {
     const i64 v = index_at(tokens, wide, i);
     return v >= 0 && v < vocab && v != padding ? (int)v : (int)vocab;
-}
-
-// Runs of all tokens: none yet.
-__global__ void __launch_bounds__(ED_THREADS) embedding_clear_kernel(int2* runs, i64 vocab) {
-    pdl_wait(runs);
-    pdl_trigger();
-    for (i64 v = (i64)blockIdx.x * ED_THREADS + threadIdx.x; v < vocab; v += (i64)gridDim.x * ED_THREADS) runs[v] = make_int2(0, 0);
 }
 
 // Few tokens: the place of each is the number of smaller ones plus that of equal ones before it.  A warp takes one token at a time.
@@ -176,7 +184,7 @@ __global__ void __launch_bounds__(RX_THREADS) radix_move_kernel(const int2* sour
         if (digit[k] >= 0) target[place[digit[k]] + warp_count[warp][digit[k]] + rank[k]] = item[k];
 }
 
-// The run of every token that is there.
+// The run of every token that is there.  (The other entries of runs are never written: who reads one looks whether the position it names holds the token.)
 __global__ void __launch_bounds__(ED_THREADS) embedding_runs_kernel(const int2* sorted, int2* runs, i64 count, i64 vocab) {
     pdl_wait(sorted, runs);
     pdl_trigger();
@@ -190,94 +198,202 @@ __global__ void __launch_bounds__(ED_THREADS) embedding_runs_kernel(const int2* 
 
 // ---- the table's gradient -------------------------------------------------------------------------------------------------------------------
 
-// Sum over sorted positions [begin, end) of VEC columns from j on, in order.
+struct TableShape {
+    i64 count, vocab, dim, stride, out_stride;
+    float scale;
+    int accumulate;
+    int lanes, slabs;                       // lanes of a team (a power of two); teams side by side that cover a row
+    unsigned long_blocks;                   // blocks that add up chunks of long runs; the others form rows
+};
+
+template <int VEC> __device__ __forceinline__ void put_floats(float* p, const float (&f)[VEC]) {
+    if constexpr (VEC == 8)
+        asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7])
+                     : "memory");
+    else if constexpr (VEC == 4)
+        *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+    else
+        *p = f[0];
+}
+template <int VEC> __device__ __forceinline__ void get_floats(const float* p, float (&f)[VEC]) {
+    if constexpr (VEC == 1) {
+        f[0] = *p;
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; e += 4) {
+            const float4 v = *reinterpret_cast<const float4*>(p + e);
+            f[e] = v.x; f[e + 1] = v.y; f[e + 2] = v.z; f[e + 3] = v.w;
+        }
+    }
+}
+
+template <int N> struct Count { static constexpr int value = N; };
+
+// VEC elements of a row of the table: 16 bytes, or 32 (fp32 from 16-bit gradients), or one element.
+template <typename O, int VEC> __device__ __forceinline__ void put_elements(O* o, const float (&f)[VEC]) {
+    if constexpr (sizeof(O) == 4) put_floats<VEC>(o, f);
+    else if constexpr (VEC == Elem<O>::VEC) store_vec(o, Elem<O>::pack(f));
+    else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) o[e] = Elem<O>::put(f[e]);
+    }
+}
+
+// The columns of one lane: ED_VECS vectors, a team's lanes side by side.
+template <int VEC>
+struct Columns {
+    i64 first, step, dim;
+    __device__ __forceinline__ Columns(const TableShape& s, int slab, int lane) : first(((i64)slab * ED_VECS * s.lanes + lane) * VEC), step((i64)s.lanes * VEC), dim(s.dim) {}
+    __device__ __forceinline__ i64 at(int k) const { return first + k * step; }
+    __device__ __forceinline__ bool in(int k) const { return at(k) < dim; }
+};
+
+// Sums over sorted positions [begin, end), in order; two positions in flight.
 template <typename T, int VEC>
-__device__ __forceinline__ void add_run(const T* grad, i64 stride, const int2* sorted, int begin, int end, i64 j, float (&sum)[VEC]) {
+__device__ __forceinline__ void add_run(const T* grad, i64 stride, const int2* sorted, int begin, int end, const Columns<VEC>& c, float (&sum)[ED_VECS][VEC]) {
     int i = begin;
-    if (VEC > 1) {
-        constexpr int N = 4;
-        for (; i + N <= end; i += N) {
-            uint4 u[N];
+    auto add = [&](auto n) {
+        constexpr int N = decltype(n)::value;
+        const T* g[N];
 #pragma unroll
-            for (int k = 0; k < N; ++k) u[k] = load_once(grad + (i64)sorted[i + k].y * stride + j);
-#pragma unroll
-            for (int k = 0; k < N; ++k) {
-                float f[Elem<T>::VEC];
-                Elem<T>::unpack(u[k], f);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) sum[e] += f[e];
-            }
-        }
-    }
-    for (; i < end; ++i) {
-        const T* g = grad + (i64)sorted[i].y * stride + j;
+        for (int p = 0; p < N; ++p) g[p] = grad + (i64)sorted[i + p].y * stride;
         if (VEC > 1) {
-            float f[Elem<T>::VEC];
-            Elem<T>::unpack(load_once(g), f);
+            uint4 u[N][ED_VECS];
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) sum[e] += f[e];
+            for (int p = 0; p < N; ++p)
+#pragma unroll
+                for (int k = 0; k < ED_VECS; ++k) if (c.in(k)) u[p][k] = load_once(g[p] + c.at(k));
+#pragma unroll
+            for (int p = 0; p < N; ++p)
+#pragma unroll
+                for (int k = 0; k < ED_VECS; ++k) {
+                    float f[Elem<T>::VEC];
+                    Elem<T>::unpack(u[p][k], f);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) sum[k][e] += f[e];
+                }
         } else {
-            sum[0] += Elem<T>::get(*g);
+            float f[N][ED_VECS];
+#pragma unroll
+            for (int p = 0; p < N; ++p)
+#pragma unroll
+                for (int k = 0; k < ED_VECS; ++k) f[p][k] = c.in(k) ? Elem<T>::get(g[p][c.at(k)]) : 0.f;
+#pragma unroll
+            for (int p = 0; p < N; ++p)
+#pragma unroll
+                for (int k = 0; k < ED_VECS; ++k) sum[k][0] += f[p][k];
         }
+        i += N;
+    };
+    while (i + 2 <= end) add(Count<2>{});
+    if (i < end) add(Count<1>{});
+}
+
+// One row's columns of a lane: scaled, added to what is there where that is asked for, rounded.
+template <typename O, int VEC>
+__device__ __forceinline__ void put_row(O* row, const Columns<VEC>& c, const float (&sum)[ED_VECS][VEC], const TableShape& s) {
+#pragma unroll
+    for (int k = 0; k < ED_VECS; ++k) {
+        if (!c.in(k)) continue;
+        O* o = row + c.at(k);
+        float f[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) f[e] = s.scale * sum[k][e];
+        if (s.accumulate) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) f[e] = fmaf(s.scale, sum[k][e], Elem<O>::get(o[e]));
+        }
+        put_elements(o, f);
     }
 }
 
-// Chunks of ED_CHUNK sorted positions: the sums of the long runs that they cut.  A run longer than a chunk holds the chunk's first or
-// its last position wherever it meets one: partial[chunk][0] belongs to the first position's run, [1] to the last one's where that is another.
-template <typename T, bool VECTORS>
-__global__ void __launch_bounds__(ED_THREADS) embedding_long_kernel(const T* grad, const int2* sorted, const int2* runs, float* partial, i64 count, i64 vocab, i64 dim, i64 stride) {
-    pdl_wait(grad, sorted, runs, partial);
-    pdl_trigger();
-    constexpr int VEC = VECTORS ? Elem<T>::VEC : 1;
-    const i64 chunk = blockIdx.x;
-    const int c0 = (int)(chunk * ED_CHUNK), c1 = (int)min(chunk * ED_CHUNK + ED_CHUNK, count);
-    const int ends[2] = {sorted[c0].x, sorted[c1 - 1].x};
-#pragma unroll
-    for (int slot = 0; slot < 2; ++slot) {
-        const int key = ends[slot];
-        if (key >= vocab || (slot == 1 && key == ends[0])) continue;
-        const int2 run = runs[key];
-        if (run.y - run.x <= ED_CHUNK) continue;
-        const int begin = max(run.x, c0), end = min(run.y, c1);
-        for (i64 j = (i64)threadIdx.x * VEC; j < dim; j += (i64)ED_THREADS * VEC) {
-            float sum[VEC] = {};
-            add_run<T, VEC>(grad, stride, sorted, begin, end, j, sum);
-            float* p = partial + (chunk * 2 + slot) * dim + j;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) p[e] = sum[e];
-        }
-    }
-}
-
-// Every row of the table.
+// Blocks up to long_blocks: chunks of ED_CHUNK sorted positions, the sums of the long runs that they cut.  A run longer than a chunk holds the chunk's first
+// or its last position wherever it meets one: partial[chunk][0] belongs to the first position's run, [1] to the last one's where that is another.
+// The others: rows of the table with no or few positions.
 template <typename T, typename O, bool VECTORS>
-__global__ void __launch_bounds__(ED_THREADS) embedding_rows_kernel(const T* grad, const int2* sorted, const int2* runs, const float* partial, O* out, i64 dim, i64 stride, i64 out_stride,
-                                                                    float scale, int accumulate) {
+__global__ void __launch_bounds__(ED_THREADS) embedding_sums_kernel(const T* grad, const int2* sorted, const int2* runs, float* partial, O* out, TableShape s) {
     pdl_wait(grad, sorted, runs, partial, out);
     pdl_trigger();
     constexpr int VEC = VECTORS ? Elem<T>::VEC : 1;
-    const i64 v = blockIdx.x;
-    const int2 run = runs[v];
-    if (run.x == run.y && accumulate) return;
-    for (i64 j = (i64)threadIdx.x * VEC; j < dim; j += (i64)ED_THREADS * VEC) {
-        float sum[VEC] = {};
-        if (run.y - run.x <= ED_CHUNK) {
-            add_run<T, VEC>(grad, stride, sorted, run.x, run.y, j, sum);
-        } else {
-            for (int chunk = run.x / ED_CHUNK; chunk <= (run.y - 1) / ED_CHUNK; ++chunk) {
-                const int slot = chunk * ED_CHUNK < run.x;                // the run's first position is not the chunk's: it is its last run
-                const float* p = partial + ((i64)chunk * 2 + slot) * dim + j;
+    const int lane = threadIdx.x & (s.lanes - 1), team = threadIdx.x / s.lanes, teams = ED_THREADS / s.lanes;
+    const bool chunks = blockIdx.x < s.long_blocks;
+    const i64 item = (i64)(chunks ? blockIdx.x : blockIdx.x - s.long_blocks) * teams + team;
+    const i64 at = s.slabs == 1 ? item : item / s.slabs;
+    const Columns<VEC> c(s, (int)(item - at * s.slabs), lane);
+    if (chunks) {
+        const i64 c0 = at * ED_CHUNK, c1 = min(c0 + ED_CHUNK, s.count);
+        if (c0 >= s.count) return;
+        const int ends[2] = {sorted[c0].x, sorted[c1 - 1].x};
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) sum[e] += p[e];
-            }
+        for (int slot = 0; slot < 2; ++slot) {
+            const int key = ends[slot];
+            if (key >= s.vocab || (slot == 1 && key == ends[0])) continue;
+            const int2 run = runs[key];
+            if (run.y - run.x <= ED_CHUNK) continue;
+            float sum[ED_VECS][VEC] = {};
+            add_run<T, VEC>(grad, s.stride, sorted, max(run.x, (int)c0), min(run.y, (int)c1), c, sum);
+            float* p = partial + (at * 2 + slot) * s.dim;
+#pragma unroll
+            for (int k = 0; k < ED_VECS; ++k) if (c.in(k)) put_floats<VEC>(p + c.at(k), sum[k]);
         }
-        O* o = out + v * out_stride + j;
+        return;
+    }
+    if (at >= s.vocab) return;
+    int2 run = runs[at];
+    if (run.x < 0 || run.x >= s.count || sorted[run.x].x != at) run = make_int2(0, 0);           // no such token
+    if (run.y - run.x > ED_CHUNK || (run.y == run.x && s.accumulate)) return;
+    float sum[ED_VECS][VEC] = {};
+    add_run<T, VEC>(grad, s.stride, sorted, run.x, run.y, c, sum);
+    put_row<O, VEC>(out + at * s.out_stride, c, sum, s);
+}
+
+// The long runs: a block per chunk and slab, at work where a long run begins in its chunk (it is the chunk's last one).  ED_SHARES teams (a block has
+// that many or more) add up a share of the run's chunks each, in order, then the shares are added in order: the same order however wide a team is.
+template <typename O, int VEC>
+__global__ void __launch_bounds__(ED_THREADS) embedding_join_kernel(const int2* sorted, const int2* runs, const float* partial, O* out, TableShape s) {
+    pdl_wait(sorted, runs, partial, out);
+    pdl_trigger();
+    __shared__ float shares[ED_THREADS * ED_VECS * VEC];           // (ED_SHARES teams of up to 32 lanes)
+    const i64 chunk = s.slabs == 1 ? blockIdx.x : blockIdx.x / s.slabs;
+    const i64 c0 = chunk * ED_CHUNK, c1 = min(c0 + ED_CHUNK, s.count);
+    const int key = sorted[c1 - 1].x;
+    if (key >= s.vocab) return;
+    const int2 run = runs[key];
+    if (run.y - run.x <= ED_CHUNK || run.x < c0) return;
+    const int lane = threadIdx.x & (s.lanes - 1), team = threadIdx.x / s.lanes, shared = ED_SHARES;
+    const Columns<VEC> c(s, (int)(blockIdx.x - chunk * s.slabs), lane);
+    const int last = (run.y - 1) / ED_CHUNK, n = last - (int)chunk + 1, per = (n + shared - 1) / shared;
+    const int begin = (int)chunk + min(team * per, n), end = (int)chunk + min((team + 1) * per, n);
+    float sum[ED_VECS][VEC] = {};
+    if (team < shared)
+#pragma unroll 2
+    for (int i = begin; i < end; ++i) {
+        // the run's first chunk holds it last, unless it begins there; every other one first
+        const float* p = partial + ((i64)i * 2 + (i == chunk && run.x > c0)) * s.dim;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const float r = accumulate ? fmaf(scale, sum[e], Elem<O>::get(o[e])) : scale * sum[e];
-            o[e] = Elem<O>::put(r);
+        for (int k = 0; k < ED_VECS; ++k) {
+            if (!c.in(k)) continue;
+            float f[VEC];
+            get_floats<VEC>(p + c.at(k), f);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum[k][e] += f[e];
         }
     }
+    // [team][vector][element][lane]: lanes side by side
+    float* mine = shares + (size_t)team * s.lanes * ED_VECS * VEC + lane;
+    if (team < shared)
+#pragma unroll
+    for (int k = 0; k < ED_VECS; ++k)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) mine[(k * VEC + e) * s.lanes] = sum[k][e];
+    __syncthreads();
+    if (team != 0) return;
+    for (int t = 1; t < min(shared, n); ++t)
+#pragma unroll
+        for (int k = 0; k < ED_VECS; ++k)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum[k][e] += shares[(size_t)t * s.lanes * ED_VECS * VEC + (k * VEC + e) * s.lanes + lane];
+    put_row<O, VEC>(out + (i64)key * s.out_stride, c, sum, s);
 }
 
 }  // namespace ef21

@@ -118,7 +118,6 @@ bool valid_table(i64 count, i64 vocab, i64 dim) {
 
 // Sorted positions and the runs of all tokens.
 ef21_status enqueue_sort(cudaStream_t st, const void* tokens, int wide, i64 count, i64 vocab, i64 padding, const EmbeddingWork& w) {
-    CU(launch(embedding_clear_kernel, grid_of(vocab, ED_THREADS * 4, SMS * 8), ED_THREADS, 0, st, 1, w.runs, vocab));
     if (count <= ED_RANK_TOKENS) {
         CU(launch(embedding_rank_kernel, grid_of(count, ED_RANK_THREADS / 32, SMS * 4), ED_RANK_THREADS, (size_t)count * sizeof(int), st, 1, tokens, wide, (int)count, vocab, padding,
                   w.sorted, w.runs));
@@ -318,10 +317,12 @@ ef21_status ef21_embedding(const void* weight_dev, int32_t dtype, int64_t vocab,
         const T* weight = static_cast<const T*>(weight_dev);
         T* out = static_cast<T*>(out_dev);
         cudaStream_t st = stream_of(cuda_stream);
-        if (aligned(weight, 16) && aligned(out, 16) && dim % VEC == 0 && weight_stride % VEC == 0)
-            CU(launch(embedding_kernel<T, true>, grid_of(count * (dim / VEC), ED_THREADS, MOST), ED_THREADS, 0, st, 1, weight, tokens_dev, out, count, vocab, dim, weight_stride, index_type, scale));
-        else
-            CU(launch(embedding_kernel<T, false>, grid_of(count * dim, ED_THREADS, MOST), ED_THREADS, 0, st, 1, weight, tokens_dev, out, count, vocab, dim, weight_stride, index_type, scale));
+        const bool vectors = aligned(weight, 16) && aligned(out, 16) && dim % VEC == 0 && weight_stride % VEC == 0;
+        const i64 slabs = ceil_div(dim, (i64)32 * ED_ROW_VECS * (vectors ? VEC : 1)), items = count * slabs;
+        if (ceil_div(items, ED_THREADS / 32) > MOST) return EF21_ERR_UNSUPPORTED;        // (1 TB of output and more)
+        const unsigned blocks = (unsigned)ceil_div(items, ED_THREADS / 32);
+        if (vectors) CU(launch(embedding_kernel<T, true>, blocks, ED_THREADS, 0, st, 1, weight, tokens_dev, out, items, (int)slabs, vocab, dim, weight_stride, index_type, scale));
+        else CU(launch(embedding_kernel<T, false>, blocks, ED_THREADS, 0, st, 1, weight, tokens_dev, out, items, (int)slabs, vocab, dim, weight_stride, index_type, scale));
         return EF21_OK;
     });
 }
@@ -346,22 +347,27 @@ ef21_status ef21_embedding_grad(const void* grad_dev, int32_t dtype, int64_t cou
     return by_dtype(dtype, [&](auto* type) -> ef21_status {
         typedef typename Pointee<decltype(type)>::type T;
         const T* grad = static_cast<const T*>(grad_dev);
-        const bool vectors = aligned(grad, 16) && dim % Elem<T>::VEC == 0 && grad_stride % Elem<T>::VEC == 0;
-        if (count > ED_CHUNK) {
-            const unsigned chunks = (unsigned)ceil_div(count, ED_CHUNK);
-            if (vectors) CU(launch(embedding_long_kernel<T, true>, chunks, ED_THREADS, 0, st, 1, grad, w.sorted, w.runs, w.partial, count, vocab, dim, grad_stride));
-            else CU(launch(embedding_long_kernel<T, false>, chunks, ED_THREADS, 0, st, 1, grad, w.sorted, w.runs, w.partial, count, vocab, dim, grad_stride));
-        }
-        auto rows = [&](auto kernel, auto* out) -> ef21_status {
-            CU(launch(kernel, (unsigned)vocab, ED_THREADS, 0, st, 1, grad, w.sorted, w.runs, w.partial, out, dim, grad_stride, out_stride, scale, accumulate));
+        auto run = [&](auto* out) -> ef21_status {
+            typedef typename Pointee<decltype(out)>::type O;
+            constexpr int VEC = Elem<T>::VEC;
+            const bool vectors = aligned(grad, 16) && dim % VEC == 0 && grad_stride % VEC == 0 && aligned(out, VEC * sizeof(O)) && out_stride % VEC == 0;
+            TableShape s{count, vocab, dim, grad_stride, out_stride, scale, accumulate, 1, 1, 0};
+            const i64 columns = dim / (vectors ? VEC : 1);
+            while (s.lanes < 32 && (i64)s.lanes * ED_VECS < columns) s.lanes *= 2;
+            s.slabs = (int)ceil_div(columns, (i64)s.lanes * ED_VECS);
+            const i64 teams = ED_THREADS / s.lanes, chunks = count > ED_CHUNK ? ceil_div(count, ED_CHUNK) : 0;
+            const i64 long_blocks = ceil_div(chunks * s.slabs, teams), row_blocks = ceil_div(vocab * s.slabs, teams);
+            if (long_blocks + row_blocks > MOST || chunks * s.slabs > MOST) return EF21_ERR_UNSUPPORTED;      // (beyond any device's memory)
+            s.long_blocks = (unsigned)long_blocks;
+            const unsigned blocks = (unsigned)(long_blocks + row_blocks);
+            if (vectors) CU(launch(embedding_sums_kernel<T, O, true>, blocks, ED_THREADS, 0, st, 1, grad, w.sorted, w.runs, w.partial, out, s));
+            else CU(launch(embedding_sums_kernel<T, O, false>, blocks, ED_THREADS, 0, st, 1, grad, w.sorted, w.runs, w.partial, out, s));
+            if (chunks == 0) return EF21_OK;
+            if (vectors) CU(launch(embedding_join_kernel<O, VEC>, (unsigned)(chunks * s.slabs), ED_THREADS, 0, st, 1, w.sorted, w.runs, w.partial, out, s));
+            else CU(launch(embedding_join_kernel<O, 1>, (unsigned)(chunks * s.slabs), ED_THREADS, 0, st, 1, w.sorted, w.runs, w.partial, out, s));
             return EF21_OK;
         };
-        if (out_dtype == EF21_DTYPE_F32) {
-            float* out = static_cast<float*>(out_dev);
-            return vectors ? rows(embedding_rows_kernel<T, float, true>, out) : rows(embedding_rows_kernel<T, float, false>, out);
-        }
-        T* out = static_cast<T*>(out_dev);
-        return vectors ? rows(embedding_rows_kernel<T, T, true>, out) : rows(embedding_rows_kernel<T, T, false>, out);
+        return out_dtype == EF21_DTYPE_F32 ? run(static_cast<float*>(out_dev)) : run(static_cast<T*>(out_dev));
     });
 }
 
