@@ -9,15 +9,19 @@
 //
 // Sorting: up to ED_RANK_TOKENS tokens by counting, for every token, those in front of it -- one launch; more by a radix sort, digits of up to nine bits.
 #pragma once
+#include <type_traits>
+
 #include "element.cuh"
 
 namespace ef21 {
 
 constexpr int ED_THREADS = 256;
+constexpr int ED_SUM_THREADS = 64;          // (a block keeps its place until its slowest team is done)
 constexpr int ED_CHUNK = 32;                // sorted positions that one team adds up
 constexpr int ED_VECS = 2;                  // vectors per lane and row
 constexpr int ED_ROW_VECS = 4;
 constexpr int ED_SHARES = ED_THREADS / 32;
+constexpr int ED_ROWS = 4;                  // rows of the table per team
 constexpr int ED_RANK_TOKENS = 8192;
 constexpr int ED_RANK_THREADS = 256;
 constexpr int RX_THREADS = 1024, RX_ITEMS = 4, RX_TILE = RX_THREADS * RX_ITEMS, RX_MAX_BITS = 9, RX_WARPS = RX_THREADS / 32;
@@ -289,6 +293,27 @@ __device__ __forceinline__ void add_run(const T* grad, i64 stride, const int2* s
     if (i < end) add(Count<1>{});
 }
 
+// A row's first gradient on its way; zeros where there is none.
+template <typename T, int VEC>
+struct First {
+    typedef typename std::conditional<(VEC > 1), uint4, float>::type Raw;
+    Raw raw[ED_VECS];
+    __device__ __forceinline__ void fetch(const T* g, const Columns<VEC>& c, bool there) {
+#pragma unroll
+        for (int k = 0; k < ED_VECS; ++k) {
+            if constexpr (VEC > 1) raw[k] = there && c.in(k) ? load_once(g + c.at(k)) : make_uint4(0u, 0u, 0u, 0u);
+            else raw[k] = there && c.in(k) ? Elem<T>::get(g[c.at(k)]) : 0.f;
+        }
+    }
+    __device__ __forceinline__ void take(float (&sum)[ED_VECS][VEC]) const {
+#pragma unroll
+        for (int k = 0; k < ED_VECS; ++k) {
+            if constexpr (VEC > 1) Elem<T>::unpack(raw[k], sum[k]);
+            else sum[k][0] = raw[k];
+        }
+    }
+};
+
 // One row's columns of a lane: scaled, added to what is there where that is asked for, rounded.
 template <typename O, int VEC>
 __device__ __forceinline__ void put_row(O* row, const Columns<VEC>& c, const float (&sum)[ED_VECS][VEC], const TableShape& s) {
@@ -307,17 +332,19 @@ __device__ __forceinline__ void put_row(O* row, const Columns<VEC>& c, const flo
     }
 }
 
-// Blocks up to long_blocks: chunks of ED_CHUNK sorted positions, the sums of the long runs that they cut.  A run longer than a chunk holds the chunk's first
+// long_blocks of the blocks: chunks of ED_CHUNK sorted positions, the sums of the long runs that they cut.  A run longer than a chunk holds the chunk's first
 // or its last position wherever it meets one: partial[chunk][0] belongs to the first position's run, [1] to the last one's where that is another.
 // The others: rows of the table with no or few positions.
 template <typename T, typename O, bool VECTORS>
-__global__ void __launch_bounds__(ED_THREADS) embedding_sums_kernel(const T* grad, const int2* sorted, const int2* runs, float* partial, O* out, TableShape s) {
+__global__ void __launch_bounds__(ED_SUM_THREADS, 12) embedding_sums_kernel(const T* grad, const int2* sorted, const int2* runs, float* partial, O* out, TableShape s) {
     pdl_wait(grad, sorted, runs, partial, out);
     pdl_trigger();
     constexpr int VEC = VECTORS ? Elem<T>::VEC : 1;
-    const int lane = threadIdx.x & (s.lanes - 1), team = threadIdx.x / s.lanes, teams = ED_THREADS / s.lanes;
-    const bool chunks = blockIdx.x < s.long_blocks;
-    const i64 item = (i64)(chunks ? blockIdx.x : blockIdx.x - s.long_blocks) * teams + team;
+    const int lane = threadIdx.x & (s.lanes - 1), team = threadIdx.x / s.lanes, teams = ED_SUM_THREADS / s.lanes;
+    // blocks of the two kinds take turns: chunks wait for one gradient after the other, rows write
+    const unsigned before = (unsigned)((unsigned long long)blockIdx.x * s.long_blocks / gridDim.x);
+    const bool chunks = before != (unsigned)((unsigned long long)(blockIdx.x + 1) * s.long_blocks / gridDim.x);
+    const i64 item = (i64)(chunks ? before : blockIdx.x - before) * teams + team;
     const i64 at = s.slabs == 1 ? item : item / s.slabs;
     const Columns<VEC> c(s, (int)(item - at * s.slabs), lane);
     if (chunks) {
@@ -338,62 +365,110 @@ __global__ void __launch_bounds__(ED_THREADS) embedding_sums_kernel(const T* gra
         }
         return;
     }
-    if (at >= s.vocab) return;
-    int2 run = runs[at];
-    if (run.x < 0 || run.x >= s.count || sorted[run.x].x != at) run = make_int2(0, 0);           // no such token
-    if (run.y - run.x > ED_CHUNK || (run.y == run.x && s.accumulate)) return;
-    float sum[ED_VECS][VEC] = {};
-    add_run<T, VEC>(grad, s.stride, sorted, run.x, run.y, c, sum);
-    put_row<O, VEC>(out + at * s.out_stride, c, sum, s);
+    // ED_ROWS rows, one after the other: their runs are looked up together, and a row's first gradient is on its way while the row before it is formed
+    const i64 first = at * ED_ROWS;
+    if (first >= s.vocab) return;
+    int2 run[ED_ROWS], head[ED_ROWS];
+#pragma unroll
+    for (int r = 0; r < ED_ROWS; ++r) {
+        run[r] = first + r < s.vocab ? runs[first + r] : make_int2(-1, -1);
+        head[r] = run[r].x >= 0 && run[r].x < s.count ? sorted[run[r].x] : make_int2(-1, 0);
+    }
+#pragma unroll
+    for (int r = 0; r < ED_ROWS; ++r) if (head[r].x != first + r) run[r] = make_int2(0, 0);          // no such token
+    First<T, VEC> next;
+    next.fetch(grad + (i64)head[0].y * s.stride, c, run[0].y > run[0].x && run[0].y - run[0].x <= ED_CHUNK);
+#pragma unroll
+    for (int r = 0; r < ED_ROWS; ++r) {
+        const int n = run[r].y - run[r].x;
+        float sum[ED_VECS][VEC];
+        next.take(sum);
+        if (r + 1 < ED_ROWS) {
+            const int m = run[(r + 1) % ED_ROWS].y - run[(r + 1) % ED_ROWS].x;
+            next.fetch(grad + (i64)head[(r + 1) % ED_ROWS].y * s.stride, c, m > 0 && m <= ED_CHUNK);
+        }
+        if (first + r >= s.vocab || n > ED_CHUNK || (n == 0 && s.accumulate)) continue;
+        if (n > 1) add_run<T, VEC>(grad, s.stride, sorted, run[r].x + 1, run[r].y, c, sum);
+        put_row<O, VEC>(out + (first + r) * s.out_stride, c, sum, s);
+    }
 }
 
-// The long runs: a block per chunk and slab, at work where a long run begins in its chunk (it is the chunk's last one).  ED_SHARES teams (a block has
-// that many or more) add up a share of the run's chunks each, in order, then the shares are added in order: the same order however wide a team is.
+// A run's first chunk holds it last (`second`), unless the run begins where the chunk does; every other one first.
+template <int VEC>
+__device__ __forceinline__ void add_partial(const float* partial, i64 chunk, bool second, const Columns<VEC>& c, float (&sum)[ED_VECS][VEC]) {
+    const float* p = partial + (chunk * 2 + second) * c.dim;
+#pragma unroll
+    for (int k = 0; k < ED_VECS; ++k) {
+        if (!c.in(k)) continue;
+        float f[VEC];
+        get_floats<VEC>(p + c.at(k), f);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sum[k][e] += f[e];
+    }
+}
+
+// The long runs, by their first chunk (a long run that begins in a chunk is its last one): a block looks through ED_SHARES chunks at once and joins, slab by slab
+// of blockIdx.y, what begins there.  ED_SHARES teams (a block has that many or more) add up a share of the run's chunks each, in order, then the
+// shares are added in order: the same order however wide a team is.
 template <typename O, int VEC>
 __global__ void __launch_bounds__(ED_THREADS) embedding_join_kernel(const int2* sorted, const int2* runs, const float* partial, O* out, TableShape s) {
     pdl_wait(sorted, runs, partial, out);
     pdl_trigger();
     __shared__ float shares[ED_THREADS * ED_VECS * VEC];           // (ED_SHARES teams of up to 32 lanes)
-    const i64 chunk = s.slabs == 1 ? blockIdx.x : blockIdx.x / s.slabs;
-    const i64 c0 = chunk * ED_CHUNK, c1 = min(c0 + ED_CHUNK, s.count);
-    const int key = sorted[c1 - 1].x;
-    if (key >= s.vocab) return;
-    const int2 run = runs[key];
-    if (run.y - run.x <= ED_CHUNK || run.x < c0) return;
-    const int lane = threadIdx.x & (s.lanes - 1), team = threadIdx.x / s.lanes, shared = ED_SHARES;
-    const Columns<VEC> c(s, (int)(blockIdx.x - chunk * s.slabs), lane);
-    const int last = (run.y - 1) / ED_CHUNK, n = last - (int)chunk + 1, per = (n + shared - 1) / shared;
-    const int begin = (int)chunk + min(team * per, n), end = (int)chunk + min((team + 1) * per, n);
-    float sum[ED_VECS][VEC] = {};
-    if (team < shared)
-#pragma unroll 2
-    for (int i = begin; i < end; ++i) {
-        // the run's first chunk holds it last, unless it begins there; every other one first
-        const float* p = partial + ((i64)i * 2 + (i == chunk && run.x > c0)) * s.dim;
-#pragma unroll
-        for (int k = 0; k < ED_VECS; ++k) {
-            if (!c.in(k)) continue;
-            float f[VEC];
-            get_floats<VEC>(p + c.at(k), f);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) sum[k][e] += f[e];
+    __shared__ int2 found[ED_SHARES];
+    __shared__ int keys[ED_SHARES];
+    if (threadIdx.x < ED_SHARES) {
+        const i64 c0 = ((i64)blockIdx.x * ED_SHARES + threadIdx.x) * ED_CHUNK;
+        int2 run = make_int2(0, 0);
+        int key = 0;
+        if (c0 < s.count) {
+            key = sorted[min(c0 + ED_CHUNK, s.count) - 1].x;
+            if (key < s.vocab) run = runs[key];
+            if (run.y - run.x <= ED_CHUNK || run.x < c0) run = make_int2(0, 0);
+        }
+        found[threadIdx.x] = run;
+        keys[threadIdx.x] = key;
+    }
+    __syncthreads();
+    const int lane = threadIdx.x & (s.lanes - 1), team = threadIdx.x / s.lanes;
+    const Columns<VEC> c(s, blockIdx.y, lane);
+    // runs of up to ED_SHARES chunks: a team each, a share being a chunk
+    if (team < ED_SHARES && found[team].y != 0) {
+        const int2 run = found[team];
+        const int chunk = run.x / ED_CHUNK, n = (run.y - 1) / ED_CHUNK - chunk + 1;
+        if (n <= ED_SHARES) {
+            float sum[ED_VECS][VEC] = {};
+#pragma unroll 4
+            for (int i = chunk; i < chunk + n; ++i) add_partial(partial, i, i == chunk && run.x > chunk * ED_CHUNK, c, sum);
+            put_row<O, VEC>(out + (i64)keys[team] * s.out_stride, c, sum, s);
         }
     }
-    // [team][vector][element][lane]: lanes side by side
-    float* mine = shares + (size_t)team * s.lanes * ED_VECS * VEC + lane;
-    if (team < shared)
+    for (int w = 0; w < ED_SHARES; ++w) {
+        const int2 run = found[w];
+        const int chunk = run.x / ED_CHUNK, n = (run.y - 1) / ED_CHUNK - chunk + 1, per = (n + ED_SHARES - 1) / ED_SHARES;
+        if (run.y == 0 || n <= ED_SHARES) continue;                // (the same in all threads)
+        const int begin = chunk + min(team * per, n), end = chunk + min((team + 1) * per, n);
+        float* mine = shares + (size_t)team * s.lanes * ED_VECS * VEC + lane;                      // [team][vector][element][lane]
+        float sum[ED_VECS][VEC] = {};
+        if (team < ED_SHARES) {
+#pragma unroll 4
+            for (int i = begin; i < end; ++i) add_partial(partial, i, i == chunk && run.x > chunk * ED_CHUNK, c, sum);
 #pragma unroll
-    for (int k = 0; k < ED_VECS; ++k)
+            for (int k = 0; k < ED_VECS; ++k)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) mine[(k * VEC + e) * s.lanes] = sum[k][e];
-    __syncthreads();
-    if (team != 0) return;
-    for (int t = 1; t < min(shared, n); ++t)
+                for (int e = 0; e < VEC; ++e) mine[(k * VEC + e) * s.lanes] = sum[k][e];
+        }
+        __syncthreads();
+        if (team == 0) {
+            for (int t = 1; t < min(ED_SHARES, n); ++t)
 #pragma unroll
-        for (int k = 0; k < ED_VECS; ++k)
+                for (int k = 0; k < ED_VECS; ++k)
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) sum[k][e] += shares[(size_t)t * s.lanes * ED_VECS * VEC + (k * VEC + e) * s.lanes + lane];
-    put_row<O, VEC>(out + (i64)key * s.out_stride, c, sum, s);
+                    for (int e = 0; e < VEC; ++e) sum[k][e] += mine[(size_t)t * s.lanes * ED_VECS * VEC + (k * VEC + e) * s.lanes];
+            put_row<O, VEC>(out + (i64)keys[w] * s.out_stride, c, sum, s);
+        }
+        __syncthreads();
+    }
 }
 
 }  // namespace ef21
