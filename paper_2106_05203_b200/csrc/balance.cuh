@@ -3,25 +3,32 @@
 //   p_t = softmax(x_t);  counts_e = tokens that chose e;  N = tokens that count;  f_e = counts_e / (K N);  P_e = 1/N sum_t p_te
 //   loss = weight E sum_e f_e P_e;   dx_tj = weight E / N p_tj (f_j - sum_e f_e p_te)
 //
-// The gradient needs the counts of the whole batch, but not P: so the choices are counted first (2 to 64 bytes a token), then one pass over the logits
-// forms the softmax, its column sums and the gradient.  f is taken about its mean: f_e - 1/E = (counts_e E - K N) / (K N E), exact in
-// whole numbers, since the sum over p takes a constant away -- a balanced router has small differences of shares that are alike.
+// The gradient needs the counts of the whole batch, but not P: so the choices are counted first (4 or 8 bytes each), then one pass over the logits
+// forms the softmax, its column sums and the gradient, and a last kernel adds the blocks' column sums up.  Few rows: one cluster does it all, every block
+// counting for itself.  f is taken about its mean: f_e - 1/E = (counts_e E - K N) / (K N E), exact in whole numbers, since the sum over p takes a constant away -- a
+// balanced router has small differences of shares that are alike.
 #pragma once
+#include "cluster.cuh"
 #include "element.cuh"
 #include "preference.cuh"
 
 namespace ef21 {
 
-constexpr int BL_THREADS = 256;
+constexpr int BL_THREADS = 256, BL_COUNT_THREADS = 1024;
 constexpr int BL_MAX_EXPERTS = 1024;
 constexpr int BL_MAX_BLOCKS = 148 * 4;
-constexpr int BL_FINISH_COLUMNS = 32, BL_FINISH_GROUPS = 32;
+constexpr int BL_FINISH_COLUMNS = 8, BL_FINISH_GROUPS = 128;
+constexpr unsigned BL_CLUSTER = 8;
+constexpr i64 BL_ONE_CHOICES = 16384, BL_ONE_LOGITS = 32768;      // up to here: one cluster
 
 struct BalanceShape {
     i64 rows;
     int experts, chosen, wide;
     i64 logit_stride, choice_stride;
     double weight;
+    int lanes;                              // that share a row (a power of two)
+    int one;                                // all blocks are one cluster: they count, and write everything
+    int whole_in, whole_out;                // rows of the logits, of the gradient begin on 16 bytes
 };
 
 struct BalanceWork { unsigned tokens, ticket; };
@@ -33,128 +40,255 @@ __global__ void __launch_bounds__(BL_THREADS) balance_clear_kernel(int* counts, 
     if (threadIdx.x == 0) { work->tokens = 0; work->ticket = 0; }
 }
 
-// Whole numbers: the order of the additions does not show.
-__global__ void __launch_bounds__(BL_THREADS) balance_count_kernel(const void* choices, const unsigned char* mask, int* counts, BalanceWork* work, BalanceShape s) {
+// Adds choices [first, all) of every `step` to here[experts], the tokens among them to n.  Whole numbers: the order of the additions does not show.
+__device__ __forceinline__ void count_choices(const void* choices, const unsigned char* mask, const BalanceShape& s, unsigned first, unsigned step, int* here, unsigned& n) {
+    const unsigned all = (unsigned)(s.rows * s.chosen), chosen = (unsigned)s.chosen;
+    for (unsigned long long base = first; base < all; base += 4ull * step) {
+        i64 e[4];
+        bool in[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const unsigned long long i = base + (unsigned long long)k * step;
+            in[k] = i < all;
+            if (!in[k]) continue;
+            const unsigned row = (unsigned)i / chosen, j = (unsigned)i - row * chosen;
+            in[k] = !mask || mask[row];
+            e[k] = index_at(choices, s.wide, (i64)row * s.choice_stride + j);
+            n += in[k] && j == 0;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) if (in[k] && e[k] >= 0 && e[k] < s.experts) atomicAdd(&here[e[k]], 1);
+    }
+}
+
+__global__ void __launch_bounds__(BL_COUNT_THREADS) balance_count_kernel(const void* choices, const unsigned char* mask, int* counts, BalanceWork* work, BalanceShape s) {
     pdl_wait(choices, mask, counts, work);
     pdl_trigger();
     __shared__ int here[BL_MAX_EXPERTS];
     __shared__ unsigned tokens;
-    for (int e = threadIdx.x; e < s.experts; e += BL_THREADS) here[e] = 0;
+    for (int e = threadIdx.x; e < s.experts; e += BL_COUNT_THREADS) here[e] = 0;
     if (threadIdx.x == 0) tokens = 0;
     __syncthreads();
     unsigned mine = 0;
-    const i64 all = s.rows * s.chosen;
-    for (i64 i = (i64)blockIdx.x * BL_THREADS + threadIdx.x; i < all; i += (i64)gridDim.x * BL_THREADS) {
-        const i64 row = i / s.chosen;
-        const int k = (int)(i - row * s.chosen);
-        if (mask && !mask[row]) continue;
-        mine += k == 0;
-        const i64 e = index_at(choices, s.wide, row * s.choice_stride + k);
-        if (e >= 0 && e < s.experts) atomicAdd(&here[e], 1);
-    }
+    count_choices(choices, mask, s, blockIdx.x * BL_COUNT_THREADS + threadIdx.x, gridDim.x * BL_COUNT_THREADS, here, mine);
     mine = __reduce_add_sync(0xffffffffu, mine);
     if ((threadIdx.x & 31) == 0 && mine) atomicAdd(&tokens, mine);
     __syncthreads();
-    for (int e = threadIdx.x; e < s.experts; e += BL_THREADS) if (here[e]) atomicAdd(counts + e, here[e]);
+    for (int e = threadIdx.x; e < s.experts; e += BL_COUNT_THREADS) if (here[e]) atomicAdd(counts + e, here[e]);
     if (threadIdx.x == 0 && tokens) atomicAdd(&work->tokens, tokens);
 }
 
-// `lanes` lanes (a power of two) share a row, lane l its columns l, l + lanes, ...: PER of them at most.
-template <typename T, int PER>
-__global__ void __launch_bounds__(BL_THREADS) balance_kernel(const T* logits, const unsigned char* mask, const int* counts, const BalanceWork* work, T* grad, float* partial, BalanceShape s, int lanes) {
-    pdl_wait(logits, mask, counts, work, grad, partial);
+// A team of s.lanes lanes takes ROWS rows at a time; lane l has PER vectors of VEC columns, lanes side by side -- of whole vectors where the number of columns
+// is a multiple of them, however the rows are aligned: the order of the additions goes by the number of columns alone.
+// LANES: 32, or 0 where s.lanes may be fewer.
+template <typename T, int VEC, int PER, int ROWS, int LANES>
+__global__ void __launch_bounds__(BL_THREADS) balance_kernel(const T* logits, const void* choices, const unsigned char* mask, int* counts, const BalanceWork* work, T* grad, float* partial,
+                                                             float* probs, float* loss, BalanceShape s) {
+    pdl_wait(logits, choices, mask, counts, work, grad, partial, probs, loss);
     pdl_trigger();
     __shared__ float column[BL_MAX_EXPERTS];
-    const int tid = threadIdx.x, lane = tid & (lanes - 1), group = tid / lanes, groups = BL_THREADS / lanes, E = s.experts;
-    const double N = (double)work->tokens, KN = N * s.chosen;
-    float apart[PER], sum[PER];
+    __shared__ int here[BL_MAX_EXPERTS];
+    __shared__ unsigned seen;
+    __shared__ double terms, scratch[BL_THREADS / 32];
+    const int tid = threadIdx.x, lanes = LANES ? LANES : s.lanes, lane = tid & (lanes - 1), group = tid / lanes, groups = BL_THREADS / lanes, E = s.experts;
+    if (s.one) {
+        for (int e = tid; e < E; e += BL_THREADS) here[e] = 0;
+        if (tid == 0) seen = 0;
+        __syncthreads();
+        unsigned mine = 0;
+        count_choices(choices, mask, s, tid, BL_THREADS, here, mine);
+        mine = __reduce_add_sync(0xffffffffu, mine);
+        if ((tid & 31) == 0 && mine) atomicAdd(&seen, mine);
+        __syncthreads();
+        if (blockIdx.x == 0) for (int e = tid; e < E; e += BL_THREADS) counts[e] = here[e];
+    }
+    const double N = (double)(s.one ? seen : work->tokens), KN = N * s.chosen;
+    auto column_of = [&](int i) { return (lane + i / VEC * lanes) * VEC + i % VEC; };
+    float apart[PER * VEC], sum[PER * VEC];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int e = lane + i * lanes;
-        apart[i] = e < E && N > 0.0 ? (float)(((double)counts[e] * E - KN) / (KN * E)) : 0.f;
+    for (int i = 0; i < PER * VEC; ++i) {
+        const int e = column_of(i);
+        apart[i] = e < E && N > 0.0 ? (float)(((double)(s.one ? here[e] : counts[e]) * E - KN) / (KN * E)) : 0.f;
         sum[i] = 0.f;
     }
     const float factor = N > 0.0 ? (float)(s.weight * E / N) : 0.f;
-    const i64 rounds = (s.rows + (i64)gridDim.x * groups - 1) / ((i64)gridDim.x * groups);
-    for (i64 k = 0; k < rounds; ++k) {                                   // (whole warps: the shuffles need every lane)
-        const i64 row = ((k * gridDim.x) + blockIdx.x) * groups + group;
-        const bool in = row < s.rows, keep = in && (!mask || mask[row]);
-        const T* x = logits + row * s.logit_stride;
-        float f[PER], top = -INFINITY;
+    const i64 step = (i64)gridDim.x * groups;
+    for (i64 row0 = (i64)blockIdx.x * groups + group; row0 - group < s.rows; row0 += step * ROWS) {     // (whole warps: the shuffles need every lane)
+        float f[ROWS][PER * VEC], top[ROWS], total[ROWS], mean[ROWS];
+        bool keep[ROWS];
+        uint4 raw[ROWS][VEC > 1 ? PER : 1];
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int e = lane + i * lanes;
-            f[i] = keep && e < E ? Elem<T>::get(x[e]) : -INFINITY;
-            top = fmaxf(top, f[i]);
+        for (int r = 0; r < ROWS; ++r) {
+            const i64 row = row0 + r * step;
+            keep[r] = row < s.rows && (!mask || mask[row]);
+            const T* x = logits + row * s.logit_stride;
+            if constexpr (VEC > 1) {
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const int at = (lane + i * lanes) * VEC;
+                    if (row >= s.rows || at >= E) continue;
+                    if (s.whole_in) { raw[r][i] = load_once(x + at); continue; }
+                    float v[VEC];
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) v[e] = Elem<T>::get(x[at + e]);
+                    raw[r][i] = Elem<T>::pack(v);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < PER; ++i) f[r][i] = row < s.rows && column_of(i) < E ? Elem<T>::get(x[column_of(i)]) : -INFINITY;
+            }
         }
-        for (int o = lanes >> 1; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const float base = top == -INFINITY ? 0.f : top;         // (a row of -inf only, or left out: all 0)
-        float total = 0.f;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) { f[i] = exp2_fast((f[i] - base) * LOG2E); total += f[i]; }
-        for (int o = lanes >> 1; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-        const float scale = !keep || total == 0.f ? 0.f : 1.f / total;
-        float mean = 0.f;
+        for (int r = 0; r < ROWS; ++r) {
+            top[r] = -INFINITY;
+            if constexpr (VEC > 1) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) { f[i] *= scale; mean = fmaf(f[i], apart[i], mean); sum[i] += f[i]; }
-        for (int o = lanes >> 1; o > 0; o >>= 1) mean += __shfl_xor_sync(0xffffffffu, mean, o);
-        if (in) {
+                for (int i = 0; i < PER; ++i) {
+                    constexpr unsigned none = Elem<T>::NEG_INF;
+                    if (!keep[r] || (lane + i * lanes) * VEC >= E) raw[r][i] = make_uint4(none, none, none, none);
+                    float v[VEC];
+                    Elem<T>::unpack(raw[r][i], v);
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int e = lane + i * lanes;
-                if (e < E) grad[row * E + e] = Elem<T>::put(keep ? factor * f[i] * (apart[i] - mean) : 0.f);
+                    for (int e = 0; e < VEC; ++e) f[r][i * VEC + e] = v[e];
+                }
+            } else if (!keep[r]) {
+#pragma unroll
+                for (int i = 0; i < PER; ++i) f[r][i] = -INFINITY;
+            }
+#pragma unroll
+            for (int i = 0; i < PER * VEC; ++i) top[r] = fmaxf(top[r], f[r][i]);
+        }
+#pragma unroll
+        for (int o = lanes >> 1; o > 0; o >>= 1) {
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], o));
+        }
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const float base = top[r] == -INFINITY ? 0.f : top[r];           // (a row of -inf only, or left out: all 0)
+            total[r] = 0.f; mean[r] = 0.f;
+#pragma unroll
+            for (int i = 0; i < PER * VEC; ++i) {
+                f[r][i] = exp2_fast((f[r][i] - base) * LOG2E);
+                total[r] += f[r][i];
+                mean[r] = fmaf(f[r][i], apart[i], mean[r]);
+            }
+        }
+#pragma unroll
+        for (int o = lanes >> 1; o > 0; o >>= 1) {
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                total[r] += __shfl_xor_sync(0xffffffffu, total[r], o);
+                mean[r] += __shfl_xor_sync(0xffffffffu, mean[r], o);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const i64 row = row0 + r * step;
+            if (row >= s.rows) continue;
+            const float scale = total[r] == 0.f ? 0.f : 1.f / total[r], about = mean[r] * scale, slope = factor * scale;
+#pragma unroll
+            for (int i = 0; i < PER * VEC; ++i) {
+                sum[i] = fmaf(f[r][i], scale, sum[i]);
+                f[r][i] = f[r][i] * slope * (apart[i] - about);
+            }
+            T* g = grad + row * E;
+            if constexpr (VEC > 1) {
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    float v[VEC];
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) v[e] = f[r][i * VEC + e];
+                    const int at = (lane + i * lanes) * VEC;
+                    if (at >= E) continue;
+                    if (s.whole_out) { store_vec(g + at, Elem<T>::pack(v)); continue; }
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) g[at + e] = Elem<T>::put(v[e]);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < PER; ++i) if (column_of(i) < E) g[column_of(i)] = Elem<T>::put(f[r][i]);
             }
         }
     }
-    // column sums of the block, group after group
-    for (int g = 0; g < groups; ++g) {
-        if (group == g) {
+    // column sums: a warp's teams by shuffles, then the block's warps one after the other
+    for (int o = lanes; o < 32; o <<= 1) {
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int e = lane + i * lanes;
-                if (e < E) column[e] = g == 0 ? sum[i] : column[e] + sum[i];
+        for (int i = 0; i < PER * VEC; ++i) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
+    }
+    for (int w = 0; w < BL_THREADS / 32; ++w) {
+        if (tid >> 5 == w && (tid & 31) < lanes) {
+#pragma unroll
+            for (int i = 0; i < PER * VEC; ++i) {
+                const int e = column_of(i);
+                if (e < E) column[e] = w == 0 ? sum[i] : column[e] + sum[i];
             }
         }
         __syncthreads();
     }
-    for (int e = tid; e < E; e += BL_THREADS) partial[(i64)blockIdx.x * E + e] = column[e];
+    if (!s.one) {
+        for (int e = tid; e < E; e += BL_THREADS) partial[(i64)blockIdx.x * E + e] = column[e];
+        return;
+    }
+    const unsigned C = cluster_blocks(), rank = cluster_rank();
+    if (C > 1) cluster_barrier();
+    double term = 0.0;
+    for (int e = (int)rank * BL_THREADS + tid; e < E; e += (int)C * BL_THREADS) {
+        double v = 0.0;
+        for (unsigned r = 0; r < C; ++r) v += (double)(C > 1 ? remote_float(&column[e], r) : column[e]);
+        v = N > 0.0 ? v / N : 0.0;
+        probs[e] = (float)v;
+        if (N > 0.0) term += (double)here[e] / KN * v;
+    }
+    double all[1] = {block_sum<BL_THREADS>(term, scratch)};
+    cluster_sums(all, &terms);                                    // (its barriers are behind the reads of column)
+    if (tid == 0 && rank == 0) *loss = (float)(s.weight * E * all[0]);
 }
 
-// Mean probabilities, 32 columns to a block, and the loss by the block that comes last (from the others' sums, in their order).
+// Mean probabilities, BL_FINISH_COLUMNS columns to a block, and the loss by the block that comes last (from the others' sums, in their order).
 __global__ void __launch_bounds__(BL_FINISH_COLUMNS * BL_FINISH_GROUPS) balance_finish_kernel(const float* partial, const int* counts, BalanceWork* work, double* part, float* probs, float* loss,
                                                                                              int blocks, int experts, int chosen, double weight) {
     pdl_wait(partial, counts, work, part, probs, loss);
     pdl_trigger();
-    __shared__ double sums[BL_FINISH_GROUPS][BL_FINISH_COLUMNS + 1];
+    __shared__ double sums[BL_FINISH_GROUPS][BL_FINISH_COLUMNS];
     __shared__ bool last;
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, e = blockIdx.x * BL_FINISH_COLUMNS + x;
-    double v = 0.0;
-    if (e < experts) for (int b = y; b < blocks; b += BL_FINISH_GROUPS) v += (double)partial[(i64)b * experts + e];
-    sums[y][x] = v;
+    const int x = threadIdx.x % BL_FINISH_COLUMNS, y = threadIdx.x / BL_FINISH_COLUMNS, e = blockIdx.x * BL_FINISH_COLUMNS + x;
+    constexpr int MOST = (BL_MAX_BLOCKS + BL_FINISH_GROUPS - 1) / BL_FINISH_GROUPS;
+    float v[MOST];
+#pragma unroll
+    for (int k = 0; k < MOST; ++k) v[k] = e < experts && y + k * BL_FINISH_GROUPS < blocks ? partial[(i64)(y + k * BL_FINISH_GROUPS) * experts + e] : 0.f;
+    double sum = 0.0;
+#pragma unroll
+    for (int k = 0; k < MOST; ++k) sum += (double)v[k];
+    sums[y][x] = sum;
     __syncthreads();
-    if (y == 0) {
+    if (threadIdx.x < 32) {                                       // four lanes to a column
+        const int col = threadIdx.x % BL_FINISH_COLUMNS, at = blockIdx.x * BL_FINISH_COLUMNS + col, share = threadIdx.x / BL_FINISH_COLUMNS;
+        constexpr int SHARE = BL_FINISH_GROUPS * BL_FINISH_COLUMNS / 32;
         const double N = (double)work->tokens;
-        double sum = 0.0;
-        for (int g = 0; g < BL_FINISH_GROUPS; ++g) sum += sums[g][x];
+        sum = 0.0;
+        for (int g = share * SHARE; g < (share + 1) * SHARE; ++g) sum += sums[g][col];
+        for (int o = BL_FINISH_COLUMNS; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         const double mean = N > 0.0 ? sum / N : 0.0;
         double term = 0.0;
-        if (e < experts) {
-            probs[e] = (float)mean;
-            if (N > 0.0) term = (double)counts[e] / (N * chosen) * mean;
+        if (at < experts && share == 0) {
+            probs[at] = (float)mean;
+            if (N > 0.0) term = (double)counts[at] / (N * chosen) * mean;
         }
         term = warp_sum(term);
-        if (x == 0) {
+        if (threadIdx.x == 0) {
             *(volatile double*)(part + blockIdx.x) = term;
             __threadfence();
             last = atomicAdd(&work->ticket, 1u) == gridDim.x - 1;
         }
     }
     __syncthreads();
-    if (last && threadIdx.x == 0) {
+    if (last && threadIdx.x < 32) {
         __threadfence();
-        double sum = 0.0;
-        for (int b = 0; b < (int)gridDim.x; ++b) sum += *(volatile double*)(part + b);
-        *loss = (float)(weight * experts * sum);
+        double all = 0.0;
+        for (int b = threadIdx.x; b < (int)gridDim.x; b += 32) all += *(volatile double*)(part + b);
+        all = warp_sum(all);
+        if (threadIdx.x == 0) *loss = (float)(weight * experts * all);
     }
 }
 

@@ -64,6 +64,22 @@ unsigned logprob_cluster(i64 rows, i64 vocab) {
     return C;
 }
 
+// ---- preference loss: which kernel --------------------------------------------------------------------------------------------------------
+
+// Blocks per pair: one where the pairs fill the device, up to eight of at least PF_PART elements each where they do not.  (A cluster's barriers cost: 512 pairs x
+// 8,191 fp32 by one block each 24 us, by eight 40.)
+struct PreferencePlan { bool by_warp, one; unsigned split, blocks; i64 losses; };
+PreferencePlan preference_plan(i64 pairs, i64 length) {
+    PreferencePlan p;
+    p.by_warp = length <= PF_WARP_LENGTH;
+    p.split = 1;
+    if (!p.by_warp) while (p.split < PF_CLUSTER && p.split * PF_PART < length && pairs * p.split * 2 <= SMS * 2) p.split *= 2;
+    p.blocks = (unsigned)(p.by_warp ? ceil_div(pairs, PF_THREADS / 32) : pairs * p.split);
+    p.one = p.blocks <= PF_CLUSTER;
+    p.losses = p.blocks / p.split;
+    return p;
+}
+
 // ---- policy loss: which kernel ------------------------------------------------------------------------------------------------------------
 
 struct PolicyWork { int* tokens; i64* counted; PolicySums* partial; };
@@ -190,7 +206,9 @@ ef21_status ef21_token_logprobs_grad(const void* logits_dev, int32_t dtype, int6
 }
 
 size_t ef21_preference_loss_workspace_bytes(int64_t pairs, int64_t length) {
-    return pairs < 1 || pairs > MOST / 2 || length < 0 || length > MOST ? 0 : align_up(sizeof(double) * (size_t)grid_of(pairs, 1, SMS * 8));
+    if (pairs < 1 || pairs > MOST / 16 || length < 0 || length > MOST) return 0;
+    const PreferencePlan p = preference_plan(pairs, length);
+    return p.one ? ALIGN : align_up(sizeof(double) * (size_t)p.losses);
 }
 
 ef21_status ef21_preference_loss(const void* logps_dev, const void* ref_dev, const uint8_t* mask_dev, int32_t dtype, int64_t pairs, int64_t length,
@@ -203,19 +221,23 @@ ef21_status ef21_preference_loss(const void* logps_dev, const void* ref_dev, con
     if (!aligned(logps_dev, e) || !aligned(ref_dev, e) || !aligned(grad_out_dev, e)) return EF21_ERR_INVALID_ARG;
     if (!workspace_fits(workspace_dev, workspace_bytes, need)) return EF21_ERR_WORKSPACE;
     double* partial = static_cast<double*>(workspace_dev);
-    const unsigned blocks = grid_of(pairs, 1, SMS * 8);
+    const PreferencePlan P = preference_plan(pairs, length);
     cudaStream_t st = stream_of(cuda_stream);
     return by_dtype(dtype, [&](auto* type) -> ef21_status {
         typedef typename Pointee<decltype(type)>::type T;
         constexpr int VEC = Elem<T>::VEC;
         const T *logps = static_cast<const T*>(logps_dev), *ref = static_cast<const T*>(ref_dev);
         T* grad = static_cast<T*>(grad_out_dev);
-        const PreferenceShape s{pairs, length, logps_stride, ref_stride, mask_stride, beta, smoothing, norm};
+        const PreferenceShape s{pairs, length, logps_stride, ref_stride, mask_stride, beta, smoothing, norm, P.split, (int)P.one};
         const bool vectors = aligned(logps, 16) && aligned(ref, 16) && aligned(grad, 16) && aligned(mask_dev, VEC) && (logps_stride - length) % VEC == 0 &&
                              (!ref || (ref_stride - length) % VEC == 0) && (!mask_dev || (mask_stride - length) % VEC == 0);
-        if (vectors) CU(launch(preference_kernel<T, true>, blocks, PF_THREADS, 0, st, 1, logps, ref, mask_dev, rewards_out_dev, grad, partial, s));
-        else CU(launch(preference_kernel<T, false>, blocks, PF_THREADS, 0, st, 1, logps, ref, mask_dev, rewards_out_dev, grad, partial, s));
-        CU(launch(preference_finish_kernel, 1, PF_THREADS, 0, st, 1, partial, loss_out_dev, (int)blocks, norm));
+        auto run = [&](auto kernel) -> ef21_status {
+            CU(launch(kernel, P.blocks, PF_THREADS, 0, st, P.one ? P.blocks : P.split, logps, ref, mask_dev, rewards_out_dev, grad, partial, loss_out_dev, s));
+            return EF21_OK;
+        };
+        if (P.by_warp) EF(vectors ? run(preference_kernel<T, true, 32>) : run(preference_kernel<T, false, 32>));
+        else EF(vectors ? run(preference_kernel<T, true, PF_THREADS>) : run(preference_kernel<T, false, PF_THREADS>));
+        if (!P.one) CU(launch(preference_finish_kernel, 1, PF_FINISH_THREADS, 0, st, 1, partial, loss_out_dev, P.losses, norm));
         return EF21_OK;
     });
 }
@@ -242,24 +264,27 @@ ef21_status ef21_policy_loss(const void* logps_dev, const void* old_dev, const v
     cudaStream_t st = stream_of(cuda_stream);
     const bool by_sequence = reduction == EF21_REDUCE_SEQUENCES, count = mask_dev && (norm == 0.0 || by_sequence);
     const unsigned count_blocks = grid_of(rows, PO_THREADS / 32, PO_MAX_BLOCKS);
-    if (count) CU(launch(policy_count_kernel, count_blocks, PO_THREADS, 0, st, 1, mask_dev, w.tokens, w.counted, rows, length, mask_stride, (int)by_sequence));
+    const i64 all = rows * length;
+    auto whole = [&](const void* p, i64 stride) { return aligned(p, 16) && (!p || rows <= 1 || stride == length); };
+    const int vec = 16 / bytes_of(dtype);
+    const bool flat = whole(logps_dev, logps_stride) && whole(old_dev, old_stride) && whole(ref_dev, ref_stride) && (!advantages_per_token || whole(advantages_dev, advantages_stride)) &&
+                      aligned(grad_out_dev, 16) && aligned(mask_dev, vec) && (!mask_dev || rows <= 1 || mask_stride == length);
+    // one cluster: its blocks count all tokens themselves, words of 4 or 8 where the arrays are flat, else one by one
+    const bool one = rows <= PO_ONE_ROWS && all <= (flat ? PO_ONE_TOKENS : PO_ONE_TOKENS / 8);
+    if (count && !one) CU(launch(policy_count_kernel, count_blocks, PO_THREADS, 0, st, 1, mask_dev, w.tokens, w.counted, rows, length, mask_stride, (int)by_sequence));
     return by_dtype(dtype, [&](auto* type) -> ef21_status {
         typedef typename Pointee<decltype(type)>::type T;
         constexpr int VEC = Elem<T>::VEC;
         const T *logps = static_cast<const T*>(logps_dev), *old = static_cast<const T*>(old_dev), *ref = static_cast<const T*>(ref_dev), *adv = static_cast<const T*>(advantages_dev);
         T* grad = static_cast<T*>(grad_out_dev);
         const PolicyShape s{rows, length, logps_stride, old_stride, ref_stride, mask_stride, advantages_stride, advantages_per_token, by_sequence,
-                            std::log1p(-clip_low), std::log1p(clip_high), (float)(1.0 - clip_low), (float)(1.0 + clip_high), (float)kl_weight, norm, (int)count_blocks};
-        auto whole = [&](const void* p, i64 stride) { return aligned(p, 16) && (!p || rows <= 1 || stride == length); };
-        const bool flat = whole(logps, logps_stride) && whole(old, old_stride) && whole(ref, ref_stride) && (!advantages_per_token || whole(adv, advantages_stride)) &&
-                          aligned(grad, 16) && aligned(mask_dev, VEC) && (!mask_dev || rows <= 1 || mask_stride == length);
-        const i64 all = rows * length;
-        const unsigned blocks = grid_of(all, (i64)PO_THREADS * (flat ? VEC : 1), PO_MAX_BLOCKS);
-        const int* tokens = count ? w.tokens : nullptr;
-        const i64* counted = count ? w.counted : nullptr;
-        if (flat) CU(launch(policy_kernel<T, true>, blocks, PO_THREADS, 0, st, 1, logps, old, ref, adv, mask_dev, tokens, counted, grad, w.partial, s));
-        else CU(launch(policy_kernel<T, false>, blocks, PO_THREADS, 0, st, 1, logps, old, ref, adv, mask_dev, tokens, counted, grad, w.partial, s));
-        CU(launch(policy_finish_kernel, 1, PO_THREADS, 0, st, 1, w.partial, terms_out_dev, (int)blocks, kl_weight));
+                            std::log1p(-clip_low), std::log1p(clip_high), (float)(1e-6 * (1.0 - std::log1p(-clip_low))), (float)(1e-6 * (1.0 + std::log1p(clip_high))), (float)(1.0 - clip_low), (float)(1.0 + clip_high), (float)kl_weight, norm, (int)count_blocks, (int)one};
+        const unsigned blocks = grid_of(all, (i64)PO_THREADS * (flat ? VEC : 1), one ? PO_CLUSTER : PO_MAX_BLOCKS);
+        const int* tokens = count && !one ? w.tokens : nullptr;
+        const i64* counted = count && !one ? w.counted : nullptr;
+        if (flat) CU(launch(policy_kernel<T, true>, blocks, PO_THREADS, 0, st, one ? blocks : 1, logps, old, ref, adv, mask_dev, tokens, counted, grad, w.partial, terms_out_dev, s));
+        else CU(launch(policy_kernel<T, false>, blocks, PO_THREADS, 0, st, one ? blocks : 1, logps, old, ref, adv, mask_dev, tokens, counted, grad, w.partial, terms_out_dev, s));
+        if (!one) CU(launch(policy_finish_kernel, 1, PO_FINISH_THREADS, 0, st, 1, w.partial, terms_out_dev, (int)blocks, (float)kl_weight));
         return EF21_OK;
     });
 }
@@ -280,30 +305,41 @@ ef21_status ef21_balance_loss(const void* logits_dev, int32_t dtype, int64_t row
     BalanceBuffers w;
     balance_layout(workspace_dev, rows, experts, w);
     cudaStream_t st = stream_of(cuda_stream);
-    const BalanceShape s{rows, (int)experts, (int)chosen, index_type, logits_stride, choices_stride, weight};
-    CU(launch(balance_clear_kernel, 1, BL_THREADS, 0, st, 1, counts_out_dev, w.work, (int)experts));
-    CU(launch(balance_count_kernel, grid_of(rows * chosen, BL_THREADS * 4, SMS * 2), BL_THREADS, 0, st, 1, choices_dev, mask_dev, counts_out_dev, w.work, s));
-    int lanes = 1;
-    while (lanes < 32 && lanes < experts) lanes *= 2;
-    const unsigned blocks = grid_of(rows, BL_THREADS / lanes, BL_MAX_BLOCKS);
-    EF(by_dtype(dtype, [&](auto* type) -> ef21_status {
+    return by_dtype(dtype, [&](auto* type) -> ef21_status {
         typedef typename Pointee<decltype(type)>::type T;
+        constexpr int V = Elem<T>::VEC;
         const T* logits = static_cast<const T*>(logits_dev);
         T* grad = static_cast<T*>(grad_out_dev);
+        const bool vectors = experts % V == 0;
+        const i64 columns = vectors ? experts / V : experts;
+        BalanceShape s{rows, (int)experts, (int)chosen, index_type, logits_stride, choices_stride, weight, 1, 0, aligned(logits, 16) && logits_stride % V == 0, aligned(grad, 16)};
+        while (s.lanes < 32 && s.lanes < columns) s.lanes *= 2;
+        s.one = rows * chosen <= BL_ONE_CHOICES && rows * experts <= BL_ONE_LOGITS;
+        const unsigned blocks = grid_of(rows, BL_THREADS / s.lanes, s.one ? BL_CLUSTER : BL_MAX_BLOCKS);
+        if (!s.one) {
+            CU(launch(balance_clear_kernel, 1, BL_THREADS, 0, st, 1, counts_out_dev, w.work, (int)experts));
+            CU(launch(balance_count_kernel, grid_of(rows * chosen, BL_COUNT_THREADS * 4, SMS * 2), BL_COUNT_THREADS, 0, st, 1, choices_dev, mask_dev, counts_out_dev, w.work, s));
+        }
         auto run = [&](auto kernel) -> ef21_status {
-            CU(launch(kernel, blocks, BL_THREADS, 0, st, 1, logits, mask_dev, counts_out_dev, w.work, grad, w.partial, s, lanes));
+            CU(launch(kernel, blocks, BL_THREADS, 0, st, s.one ? blocks : 1, logits, choices_dev, mask_dev, counts_out_dev, w.work, grad, w.partial, probs_out_dev, loss_out_dev, s));
             return EF21_OK;
         };
-        if (experts <= 32) return run(balance_kernel<T, 1>);
-        if (experts <= 64) return run(balance_kernel<T, 2>);
-        if (experts <= 128) return run(balance_kernel<T, 4>);
-        if (experts <= 256) return run(balance_kernel<T, 8>);
-        if (experts <= 512) return run(balance_kernel<T, 16>);
-        return run(balance_kernel<T, 32>);
-    }));
-    CU(launch(balance_finish_kernel, (unsigned)ceil_div(experts, BL_FINISH_COLUMNS), BL_FINISH_COLUMNS * BL_FINISH_GROUPS, 0, st, 1, w.partial, counts_out_dev, w.work, w.part,
-              probs_out_dev, loss_out_dev, (int)blocks, (int)experts, (int)chosen, weight));
-    return EF21_OK;
+        // rows in flight per team: 16 to 32 values per lane
+        const bool full = s.lanes == 32;
+        if (vectors) {
+            if (columns <= 32) EF(full ? run(balance_kernel<T, V, 1, 16 / V, 32>) : run(balance_kernel<T, V, 1, 16 / V, 0>));
+            else if (columns <= 64) EF(run(balance_kernel<T, V, 2, 1, 32>));
+            else if (columns <= 128) EF(run(balance_kernel<T, V, 4, 1, 32>));
+            else if constexpr (V == 4) EF(run(balance_kernel<T, V, 8, 1, 32>));
+        } else {
+            if (columns <= 32) EF(full ? run(balance_kernel<T, 1, 1, 4, 32>) : run(balance_kernel<T, 1, 1, 4, 0>));
+            else if (columns <= 128) EF(run(balance_kernel<T, 1, 4, 4, 32>));
+            else EF(run(balance_kernel<T, 1, 32, 1, 32>));
+        }
+        if (!s.one) CU(launch(balance_finish_kernel, (unsigned)ceil_div(experts, BL_FINISH_COLUMNS), BL_FINISH_COLUMNS * BL_FINISH_GROUPS, 0, st, 1, w.partial, counts_out_dev, w.work, w.part,
+                              probs_out_dev, loss_out_dev, (int)blocks, (int)experts, (int)chosen, weight));
+        return EF21_OK;
+    });
 }
 
 ef21_status ef21_embedding(const void* weight_dev, int32_t dtype, int64_t vocab, int64_t dim, int64_t weight_stride, const void* tokens_dev, int32_t index_type, int64_t count, float scale,

@@ -4,9 +4,11 @@
 //   loss = sum w (pg + weight kl),  w = 1 / tokens, or 1 / (rows with tokens * tokens of the row), 0 where the mask leaves a token out
 //   d loss / d lp = w (-A r [not clipped] - weight (exp(delta) - 1));  clipped: A > 0 and r > 1 + hi, or A < 0 and r < 1 - lo
 //
-// Two kernels over the data: the tokens are counted (the mask alone, 1 of 14 to 21 bytes), then everything else is one pass.  Which side of a border a
-// ratio lies on is decided on d, in 64 bits: the gradient jumps there.
+// The tokens are counted first (the mask alone, 1 of 14 to 21 bytes), then everything else is one pass, and a third kernel adds up the blocks' terms.
+// Few tokens: one cluster does it all, every block counting for itself.  Which side of a border a ratio lies on is decided on d, in 64 bits where 32
+// could err: the gradient jumps there.
 #pragma once
+#include "cluster.cuh"
 #include "element.cuh"
 #include "preference.cuh"
 
@@ -14,6 +16,10 @@ namespace ef21 {
 
 constexpr int PO_THREADS = 256;
 constexpr int PO_MAX_BLOCKS = 148 * 8;
+constexpr int PO_FINISH_THREADS = 1024;
+constexpr i64 PO_ONE_TOKENS = 16384;         // up to here (and PO_ONE_ROWS rows): one cluster of up to eight blocks
+constexpr int PO_ONE_ROWS = 1024;
+constexpr unsigned PO_CLUSTER = 8;
 
 struct PolicyShape {
     i64 rows, length;
@@ -21,10 +27,12 @@ struct PolicyShape {
     int adv_per_token;
     int by_sequence;
     double log_low, log_high;                // log(1 - lo), log(1 + hi)
+    float near_low, near_high;               // how close to these a difference in 32 bits says nothing
     float low, high;                         // 1 - lo, 1 + hi
     float kl_weight;
     double norm;                             // 0: counted
     int count_blocks;
+    int one;                                 // all blocks are one cluster: they count, and write the terms
 };
 
 // exp(x) - 1 - x >= 0, to a few units in the last place: the series about 0, where the difference would lose everything.
@@ -35,6 +43,10 @@ __device__ __forceinline__ float exp_minus_line(float x) {
     p = fmaf(p, x, 1.f / 720.f); p = fmaf(p, x, 1.f / 120.f); p = fmaf(p, x, 1.f / 24.f); p = fmaf(p, x, 1.f / 6.f); p = fmaf(p, x, 0.5f);
     return p * x * x;
 }
+
+// Bytes of a mask word that are not 0.
+__device__ __forceinline__ int count_bytes(unsigned w) { return __popc(__vcmpne4(w, 0u) & 0x01010101u); }
+__device__ __forceinline__ int count_bytes(unsigned long long w) { return count_bytes((unsigned)w) + count_bytes((unsigned)(w >> 32)); }
 
 // Tokens of every row, and per block how many tokens (by_sequence: rows that have any) its rows hold.
 __global__ void __launch_bounds__(PO_THREADS) policy_count_kernel(const unsigned char* mask, int* tokens, i64* partial, i64 rows, i64 length, i64 stride, int by_sequence) {
@@ -49,10 +61,12 @@ __global__ void __launch_bounds__(PO_THREADS) policy_count_kernel(const unsigned
         const i64 vectors = (length - head) / 16, tail = head + vectors * 16;
         int n = 0;
         if (lane < head) n += m[lane] != 0;
-        for (i64 v = lane; v < vectors; v += 32) {
-            const uint4 u = *reinterpret_cast<const uint4*>(m + head + v * 16);
-            n += __popc(__vcmpne4(u.x, 0u) & 0x01010101u) + __popc(__vcmpne4(u.y, 0u) & 0x01010101u) + __popc(__vcmpne4(u.z, 0u) & 0x01010101u) +
-                 __popc(__vcmpne4(u.w, 0u) & 0x01010101u);
+        for (i64 v = lane; v < vectors; v += 4 * 32) {
+            uint4 u[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) u[k] = v + k * 32 < vectors ? *reinterpret_cast<const uint4*>(m + head + (v + k * 32) * 16) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) n += count_bytes(u[k].x) + count_bytes(u[k].y) + count_bytes(u[k].z) + count_bytes(u[k].w);
         }
         if (tail + lane < length) n += m[tail + lane] != 0;
         n = __reduce_add_sync(0xffffffffu, n);
@@ -70,35 +84,87 @@ __global__ void __launch_bounds__(PO_THREADS) policy_count_kernel(const unsigned
 
 struct PolicySums { double pg = 0.0, kl = 0.0, clipped = 0.0; };
 
-// One token of weight w; adds its terms and returns its gradient.
-__device__ __forceinline__ float policy_token(float lp, float old, float ref, bool has_ref, float A, float w, const PolicyShape& s, float& pg, float& kl, float& clip) {
-    const double d = (double)lp - (double)old;
-    const bool clipped = (A > 0.f && d > s.log_high) || (A < 0.f && d < s.log_low);
-    const float r = clipped ? (A > 0.f ? s.high : s.low) : (A == 0.f ? 0.f : expf(lp - old));
-    float g = clipped ? 0.f : -A * r;
-    pg -= w * (r * A);
-    clip += clipped ? w : 0.f;
+__device__ __forceinline__ void write_terms(float* terms, double pg, double kl, double clipped, double kl_weight) {
+    terms[0] = (float)(kl_weight == 0.0 ? pg : pg + kl_weight * kl);
+    terms[1] = (float)pg; terms[2] = (float)kl; terms[3] = (float)clipped;
+}
+
+// One token: its terms without their weight are added to pg, kl and clip, its gradient (without the weight) returned.
+__device__ __forceinline__ float policy_token(float lp, float old, float ref, bool has_ref, float A, const PolicyShape& s, float& pg, float& kl, float& clip) {
+    const float d = lp - old;
+    // beyond the border that counts for the sign of A?  The fp32 difference is good to half a step of its own; next to the border the exact one is taken
+    const bool up = A > 0.f;
+    const double border = up ? s.log_high : s.log_low;
+    const float past = d - (float)border;
+    bool clipped = up ? past > 0.f : past < 0.f;
+    if (fabsf(past) <= (up ? s.near_high : s.near_low)) {
+        const double exact = (double)lp - (double)old;
+        clipped = up ? exact > border : exact < border;
+    }
+    clipped = clipped && A != 0.f;
+    const float r = clipped ? (up ? s.high : s.low) : A == 0.f ? 0.f : expf(d), gain = r * A;
+    float g = clipped ? 0.f : -gain;
+    pg -= gain;
+    clip += clipped ? 1.f : 0.f;
     if (has_ref) {
         const float delta = ref - lp, k = exp_minus_line(delta);
-        kl += w * k;
+        kl += k;
         g -= s.kl_weight * (k + delta);
     }
-    return w * g;
+    return g;
 }
 
 // FLAT: all arrays are contiguous, a vector of VEC tokens may run over the end of a row.  Otherwise token by token, any strides.
 template <typename T, bool FLAT>
 __global__ void __launch_bounds__(PO_THREADS) policy_kernel(const T* logps, const T* old, const T* ref, const T* adv, const unsigned char* mask, const int* tokens, const i64* counted,
-                                                            T* grad, PolicySums* partial, PolicyShape s) {
-    pdl_wait(logps, old, ref, adv, mask, tokens, counted, grad, partial);
+                                                            T* grad, PolicySums* partial, float* terms, PolicyShape s) {
+    pdl_wait(logps, old, ref, adv, mask, tokens, counted, grad, partial, terms);
     pdl_trigger();
     constexpr int VEC = FLAT ? Elem<T>::VEC : 1;
     typedef typename MaskWord<Elem<T>::VEC>::type Word;
     __shared__ double scratch[PO_THREADS / 32];
+    __shared__ int row_tokens[PO_ONE_ROWS], seen;
     const int tid = threadIdx.x;
+    const bool in_block = s.one && mask && (s.norm == 0.0 || s.by_sequence);
+    if (in_block) {
+        if (tid == 0) seen = 0;
+        for (int r = tid; r < (int)s.rows; r += PO_THREADS) row_tokens[r] = 0;
+        __syncthreads();
+        const unsigned all = (unsigned)(s.rows * s.length), length = (unsigned)s.length, words = FLAT ? all / Elem<T>::VEC : 0u;
+        int n = 0;                                                     // tokens, whole numbers: any order
+        auto add = [&](unsigned row, int k) { if (s.by_sequence) atomicAdd(&row_tokens[row], k); else n += k; };
+        if constexpr (FLAT) {
+            for (unsigned base = tid; base < words; base += 4 * PO_THREADS) {
+                Word w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = base + k * PO_THREADS < words ? reinterpret_cast<const Word*>(mask)[base + k * PO_THREADS] : (Word)0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (w[k] == 0) continue;
+                    const unsigned i = (base + k * PO_THREADS) * Elem<T>::VEC, row = s.by_sequence ? i / length : 0u;
+                    if (!s.by_sequence || i + Elem<T>::VEC <= (row + 1) * length) {
+                        add(row, count_bytes(w[k]));
+                    } else {
+                        for (int e = 0; e < Elem<T>::VEC; ++e) if (w[k] >> (8 * e) & 255u) add((i + e) / length, 1);
+                    }
+                }
+            }
+        }
+        for (unsigned i = words * Elem<T>::VEC + tid; i < all; i += PO_THREADS) {
+            const unsigned row = i / length;
+            if (mask[(i64)row * s.mask_stride + (i - row * length)]) add(row, 1);
+        }
+        __syncthreads();
+        if (s.by_sequence) for (int r = tid; r < (int)s.rows; r += PO_THREADS) n += row_tokens[r] > 0;
+        n = __reduce_add_sync(0xffffffffu, n);
+        if ((tid & 31) == 0 && n) atomicAdd(&seen, n);
+        __syncthreads();
+    }
     double norm = s.norm;
     if (norm == 0.0) {
-        if (counted) {
+        if (in_block) {
+            norm = (double)seen;
+        } else if (counted) {
             double n = 0.0;
             for (int b = tid; b < s.count_blocks; b += PO_THREADS) n += (double)counted[b];
             norm = block_sum<PO_THREADS>(n, scratch);
@@ -109,67 +175,99 @@ __global__ void __launch_bounds__(PO_THREADS) policy_kernel(const T* logps, cons
     const float inverse = norm > 0.0 ? (float)(1.0 / norm) : 0.f;
     auto weight = [&](i64 row) {
         if (!s.by_sequence) return inverse;
-        const i64 n = tokens ? (i64)tokens[row] : s.length;
-        return n > 0 ? inverse / (float)n : 0.f;
+        const i64 n = in_block ? (i64)row_tokens[row] : tokens ? (i64)tokens[row] : s.length;
+        return n > 0 ? __fdividef(inverse, (float)n) : 0.f;
     };
     PolicySums sums;
     const i64 all = s.rows * s.length, vectors = all / VEC, step = (i64)gridDim.x * PO_THREADS;
+    const bool small = all < (1ll << 31);                              // (a division of 32 bits)
     auto token = [&](i64 i) {                                       // one token, any strides
-        const i64 row = i / s.length, t = i - row * s.length;
+        const i64 row = small ? (i64)((unsigned)i / (unsigned)s.length) : i / s.length, t = i - row * s.length;
         T* g = grad + i;
         if (mask && !mask[row * s.mask_stride + t]) { *g = Elem<T>::put(0.f); return; }
         float pg = 0.f, kl = 0.f, clip = 0.f;
-        const float A = Elem<T>::get(adv[row * s.adv_stride + (s.adv_per_token ? t : 0)]);
+        const float A = Elem<T>::get(adv[row * s.adv_stride + (s.adv_per_token ? t : 0)]), weighs = weight(row);
         const float v = policy_token(Elem<T>::get(logps[row * s.logp_stride + t]), Elem<T>::get(old[row * s.old_stride + t]),
-                                     ref ? Elem<T>::get(ref[row * s.ref_stride + t]) : 0.f, ref != nullptr, A, weight(row), s, pg, kl, clip);
-        *g = Elem<T>::put(v);
-        sums.pg += (double)pg; sums.kl += (double)kl; sums.clipped += (double)clip;
+                                     ref ? Elem<T>::get(ref[row * s.ref_stride + t]) : 0.f, ref != nullptr, A, s, pg, kl, clip);
+        *g = Elem<T>::put(weighs * v);
+        sums.pg += (double)(weighs * pg); sums.kl += (double)(weighs * kl); sums.clipped += (double)(weighs * clip);
     };
-    for (i64 v = (i64)blockIdx.x * PO_THREADS + tid; v < vectors; v += step) {
-        const i64 i = v * VEC;
-        if (!FLAT) { token(i); continue; }
-        const Word w = mask ? *reinterpret_cast<const Word*>(mask + i) : ~(Word)0;
-        if (w == 0) { store_vec(grad + i, make_uint4(0u, 0u, 0u, 0u)); continue; }
-        float x[Elem<T>::VEC], o[Elem<T>::VEC], f[Elem<T>::VEC], A[Elem<T>::VEC], g[Elem<T>::VEC];
-        const uint4 ux = load_once(logps + i), uo = load_once(old + i), uf = ref ? load_once(ref + i) : make_uint4(0u, 0u, 0u, 0u);
-        const uint4 ua = s.adv_per_token ? load_once(adv + i) : make_uint4(0u, 0u, 0u, 0u);
-        i64 row = i / s.length, left = s.length - (i - row * s.length);          // tokens of the row from here on
-        Elem<T>::unpack(ux, x); Elem<T>::unpack(uo, o); Elem<T>::unpack(uf, f); Elem<T>::unpack(ua, A);
-        float rowA = s.adv_per_token ? 0.f : Elem<T>::get(adv[row * s.adv_stride]), rowW = weight(row);
-        float pg = 0.f, kl = 0.f, clip = 0.f;
+    auto word = [&](i64 v) { return !FLAT || v >= vectors ? (Word)0 : mask ? *reinterpret_cast<const Word*>(mask + v * VEC) : ~(Word)0; };
+    const i64 start = (i64)blockIdx.x * PO_THREADS + tid;
+    if constexpr (!FLAT) {
+        for (i64 v = start; v < vectors; v += step) token(v);
+    } else if (start < vectors) {
+        Word next = word(start);
+        // row and position of the vector, carried along
+        const i64 skip_rows = step * VEC / s.length, skip = step * VEC - skip_rows * s.length;
+        i64 row = start * VEC / s.length, t = start * VEC - row * s.length;
+        for (i64 v = start; v < vectors; v += step) {
+            const i64 i = v * VEC;
+            const Word w = next;
+            next = word(v + step);                                     // (on its way while this one's tokens are)
+            if (w == 0) {
+                store_vec(grad + i, make_uint4(0u, 0u, 0u, 0u));
+            } else {
+                float x[VEC], o[VEC], f[VEC], A[VEC], g[VEC];
+                const uint4 ux = load_once(logps + i), uo = load_once(old + i), uf = ref ? load_once(ref + i) : make_uint4(0u, 0u, 0u, 0u);
+                const uint4 ua = s.adv_per_token ? load_once(adv + i) : make_uint4(0u, 0u, 0u, 0u);
+                float weighs = weight(row);
+                Elem<T>::unpack(ux, x); Elem<T>::unpack(uo, o); Elem<T>::unpack(uf, f); Elem<T>::unpack(ua, A);
+                if (!s.adv_per_token) {
+                    const float a = Elem<T>::get(adv[row * s.adv_stride]);
 #pragma unroll
-        for (int e = 0; e < Elem<T>::VEC; ++e) {
-            if (left == 0) {
-                ++row; left = s.length;
-                if (!s.adv_per_token) rowA = Elem<T>::get(adv[row * s.adv_stride]);
-                rowW = weight(row);
+                    for (int e = 0; e < VEC; ++e) A[e] = a;
+                }
+                float pg = 0.f, kl = 0.f, clip = 0.f;
+                if (t + VEC <= s.length) {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) g[e] = (w >> (8 * e) & 255u) != 0 ? weighs * policy_token(x[e], o[e], f[e], ref != nullptr, A[e], s, pg, kl, clip) : 0.f;
+                } else {                                               // it runs over the end of a row
+                    i64 at = row, left = s.length - t;
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        if (left == 0) {
+                            sums.pg += (double)(weighs * pg); sums.kl += (double)(weighs * kl); sums.clipped += (double)(weighs * clip);
+                            pg = kl = clip = 0.f;
+                            ++at; left = s.length;
+                            weighs = weight(at);
+                        }
+                        --left;
+                        const float a = s.adv_per_token ? A[e] : Elem<T>::get(adv[at * s.adv_stride]);
+                        g[e] = (w >> (8 * e) & 255u) != 0 ? weighs * policy_token(x[e], o[e], f[e], ref != nullptr, a, s, pg, kl, clip) : 0.f;
+                    }
+                }
+                store_vec(grad + i, Elem<T>::pack(g));
+                sums.pg += (double)(weighs * pg); sums.kl += (double)(weighs * kl); sums.clipped += (double)(weighs * clip);
             }
-            --left;
-            g[e] = (w >> (8 * e) & 255u) != 0 ? policy_token(x[e], o[e], f[e], ref != nullptr, s.adv_per_token ? A[e] : rowA, rowW, s, pg, kl, clip) : 0.f;
+            row += skip_rows; t += skip;
+            if (t >= s.length) { t -= s.length; ++row; }
         }
-        store_vec(grad + i, Elem<T>::pack(g));
-        sums.pg += (double)pg; sums.kl += (double)kl; sums.clipped += (double)clip;
     }
     if (FLAT && blockIdx.x == 0 && vectors * VEC + tid < all) token(vectors * VEC + tid);
     sums.pg = block_sum<PO_THREADS>(sums.pg, scratch);
     sums.kl = block_sum<PO_THREADS>(sums.kl, scratch);
     sums.clipped = block_sum<PO_THREADS>(sums.clipped, scratch);
+    if (s.one) {
+        __shared__ double mine[3];
+        double all_sums[3] = {sums.pg, sums.kl, sums.clipped};
+        cluster_sums(all_sums, mine);
+        if (tid == 0 && cluster_rank() == 0) write_terms(terms, all_sums[0], all_sums[1], all_sums[2], (double)s.kl_weight);
+        return;
+    }
     if (tid == 0) partial[blockIdx.x] = sums;
 }
 
-__global__ void __launch_bounds__(PO_THREADS) policy_finish_kernel(const PolicySums* partial, float* terms, int blocks, double kl_weight) {
+__global__ void __launch_bounds__(PO_FINISH_THREADS) policy_finish_kernel(const PolicySums* partial, float* terms, int blocks, float kl_weight) {
     pdl_wait(partial, terms);
     pdl_trigger();
-    __shared__ double scratch[PO_THREADS / 32];
+    __shared__ double scratch[PO_FINISH_THREADS / 32];
     PolicySums v;
-    for (int b = threadIdx.x; b < blocks; b += PO_THREADS) { v.pg += partial[b].pg; v.kl += partial[b].kl; v.clipped += partial[b].clipped; }
-    v.pg = block_sum<PO_THREADS>(v.pg, scratch);
-    v.kl = block_sum<PO_THREADS>(v.kl, scratch);
-    v.clipped = block_sum<PO_THREADS>(v.clipped, scratch);
-    if (threadIdx.x == 0) {
-        terms[0] = (float)(kl_weight == 0.0 ? v.pg : v.pg + kl_weight * v.kl);
-        terms[1] = (float)v.pg; terms[2] = (float)v.kl; terms[3] = (float)v.clipped;
-    }
+    for (int b = threadIdx.x; b < blocks; b += PO_FINISH_THREADS) { v.pg += partial[b].pg; v.kl += partial[b].kl; v.clipped += partial[b].clipped; }
+    v.pg = block_sum<PO_FINISH_THREADS>(v.pg, scratch);
+    v.kl = block_sum<PO_FINISH_THREADS>(v.kl, scratch);
+    v.clipped = block_sum<PO_FINISH_THREADS>(v.clipped, scratch);
+    if (threadIdx.x == 0) write_terms(terms, v.pg, v.kl, v.clipped, (double)kl_weight);
 }
 
 }  // namespace ef21

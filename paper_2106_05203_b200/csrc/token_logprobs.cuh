@@ -6,6 +6,7 @@
 // Both directions read every logit once; the forward pass carries the running maximum m and the sum of 2^((x - m) c), c = s log2 e.  The maximum
 // is subtracted before anything is multiplied: a row that a mask of the type's lowest value leaves nothing of must not overflow.
 #pragma once
+#include "cluster.cuh"
 #include "element.cuh"
 
 namespace ef21 {
@@ -144,17 +145,13 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_block_kernel(const T* log
     }
     if (C > 1) {
         if (tid == 0) whole = r;
-        asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+        cluster_barrier();
         if (rank == 0 && tid < 32) {
             Running w;
-            if (tid < (int)C) {
-                unsigned at = (unsigned)__cvta_generic_to_shared(&whole), remote;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(at), "r"(tid));
-                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(w.m), "=f"(w.s) : "r"(remote) : "memory");
-            }
+            if (tid < (int)C) { w.m = remote_float(&whole.m, tid); w.s = remote_float(&whole.s, tid); }
             r = warp_merge(w, c);
         }
-        asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");      // nobody leaves while it is read
+        cluster_barrier();                                     // nobody leaves while it is read
     }
     if (tid == 0 && rank == 0) write_logprob(r, xt, inside, s.scale, c, logps + row, lse + row);
 }
