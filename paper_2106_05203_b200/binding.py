@@ -22,6 +22,7 @@ from .build import call_built_for
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libef21.so")
 CALL_PATH = os.path.join(_HERE, "_topk_call.so")
+MODEL_CALL_PATH = os.path.join(_HERE, "_model_call.so")
 
 EF21_OK = 0
 STATUS_NAMES = {0: "EF21_OK", 1: "EF21_ERR_INVALID_ARG", 2: "EF21_ERR_STATE", 3: "EF21_ERR_WORKSPACE",
@@ -109,24 +110,55 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     return lib
 
 
+def _load_module(name: str, path: str):
+    spec = importlib.util.spec_from_file_location(name, path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    if module.built_for != call_built_for():
+        raise ImportError(f"{path} was built for {module.built_for}, this is {call_built_for()}")
+    return module
+
+
+def _address(entry) -> int:
+    return ctypes.cast(entry, _vp).value
+
+
 def _load_call(path: str = CALL_PATH):
     """The native form of topk() for the usual arguments (csrc/topk_call.cpp).  Where it is missing or does not fit this torch, every
     call of topk() is the general one, 4 us slower on short vectors."""
     try:
-        spec = importlib.util.spec_from_file_location("_topk_call", path)
-        module = importlib.util.module_from_spec(spec)
-        spec.loader.exec_module(module)
-        if module.built_for != call_built_for():
-            raise ImportError(f"{path} was built for {module.built_for}, this is {call_built_for()}")
+        module = _load_module("_topk_call", path)
     except (ImportError, OSError, AttributeError) as e:
         warnings.warn(f"topk() without its native call ({e}): build it with `python -m paper_2106_05203_b200.build`", RuntimeWarning, stacklevel=2)
         return lambda v, k: None
-    module.set_entry(*(ctypes.cast(f, _vp).value for f in (_lib.ef21_topk_workspace_bytes, _lib.ef21_topk)))
+    module.set_entry(*(_address(f) for f in (_lib.ef21_topk_workspace_bytes, _lib.ef21_topk)))
     return module.topk
+
+
+class _GeneralCalls:
+    """In place of the native calls of a language model's worker: every call is the general one."""
+
+    def __getattr__(self, name):
+        return lambda *args: None
+
+
+def _load_model_calls(path: str = MODEL_CALL_PATH):
+    """The native forms of token_logprobs() to embedding_grad() for the usual arguments (csrc/model_call.cpp).  Where they are missing or do not fit this
+    torch, every call is the general one, some 10 us slower on small batches."""
+    try:
+        module = _load_module("_model_call", path)
+        module.set_entries(*(_address(getattr(_lib, f)) for f in (
+            "ef21_token_logprobs", "ef21_token_logprobs_grad", "ef21_preference_loss_workspace_bytes", "ef21_preference_loss", "ef21_policy_loss_workspace_bytes",
+            "ef21_policy_loss", "ef21_balance_loss_workspace_bytes", "ef21_balance_loss", "ef21_embedding", "ef21_embedding_grad_workspace_bytes", "ef21_embedding_grad")))
+    except (ImportError, OSError, AttributeError, TypeError) as e:
+        warnings.warn(f"losses and embedding without their native calls ({e}): build them with `python -m paper_2106_05203_b200.build`", RuntimeWarning, stacklevel=2)
+        return _GeneralCalls()
+    return module
 
 
 _lib = load_library()
 _topk_call = _load_call()
+_model_calls = _load_model_calls()
 
 
 def _check(status: int, where: str) -> None:
@@ -480,6 +512,13 @@ class BalanceLoss(NamedTuple):
     grad: torch.Tensor          # [R, E]: of the logits, in their type
 
 
+def _native(out, where: str):
+    """What a native call gave: its result, or the library's refusal."""
+    if type(out) is int:
+        raise Ef21Error(out, where)
+    return out
+
+
 def _type_of(t: torch.Tensor, name: str) -> int:
     code = DTYPES.get(t.dtype)
     if code is None:
@@ -530,6 +569,8 @@ def _same_device(*tensors: Optional[torch.Tensor]) -> torch.device:
 def _elsewhere(device: torch.device, stream: Optional[torch.cuda.Stream]):
     """None where the call's stream and device are the current ones; else the context in which they are."""
     if stream is not None:
+        if not isinstance(stream, torch.cuda.Stream):
+            raise TypeError(f"stream must be a torch.cuda.Stream, not {type(stream).__name__}")
         if stream.device != device:
             raise ValueError(f"tensors on {device}, a stream of {stream.device}")
         return torch.cuda.stream(stream)
@@ -572,6 +613,10 @@ def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, scale: float = 1
 
     logits[rows, vocab] or [batch, length, vocab], with any strides between rows: score whole sequences as
     token_logprobs(logits[:, :-1], tokens[:, 1:]), no copy is made.  Where the target is `ignore`, the row is not read and both are 0."""
+    if stream is None:
+        result = _model_calls.token_logprobs(logits, targets, scale, ignore)                        # None: not one of the usual calls
+        if result is not None:
+            return _native(result, "ef21_token_logprobs")
     dtype, index = _type_of(logits, "logits"), _index_type_of(targets, "targets")
     batch, length, vocab, batch_stride, row_stride = _logit_rows(logits, "logits")
     _targets_fit(targets, logits)
@@ -592,6 +637,10 @@ def token_logprobs_grad(logits: torch.Tensor, targets: torch.Tensor, lse: torch.
                         out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """The logits' gradient, given that of the log-probabilities: grad[...] and lse[...] are contiguous fp32 of targets' shape, the other arguments as
     they were for token_logprobs.  out (of logits' shape and type) may be the logits themselves, which are then overwritten."""
+    if stream is None and out is None:
+        result = _model_calls.token_logprobs_grad(logits, targets, lse, grad, scale, ignore)                        # None: not one of the usual calls
+        if result is not None:
+            return _native(result, "ef21_token_logprobs_grad")
     dtype, index = _type_of(logits, "logits"), _index_type_of(targets, "targets")
     batch, length, vocab, batch_stride, row_stride = _logit_rows(logits, "logits")
     _targets_fit(targets, logits)
@@ -625,6 +674,10 @@ def preference_loss(logps: torch.Tensor, ref_logps: Optional[torch.Tensor] = Non
     """Logistic loss of paired log ratios with its gradient: logps[2 P, T] are the log-probabilities of the chosen answers' tokens, then of the rejected
     ones', ref_logps those under the reference (None: 0), mask[2 P, T] the tokens that count (None: all).  The loss is the sum over pairs over `norm`
     (None: P)."""
+    if stream is None:
+        result = _model_calls.preference_loss(logps, ref_logps, mask, beta, smoothing, norm)                        # None: not one of the usual calls
+        if result is not None:
+            return PreferenceLoss._make(_native(result, "ef21_preference_loss"))
     dtype = _type_of(logps, "logps")
     if logps.dim() != 2 or logps.shape[0] % 2 or logps.shape[0] == 0:
         raise ValueError(f"logps must be [2 pairs, length], not {tuple(logps.shape)}")
@@ -655,6 +708,10 @@ def policy_loss(logps: torch.Tensor, old_logps: torch.Tensor, advantages: torch.
     """Clipped policy loss with a KL term, with its gradient: logps[R, T], old_logps and ref_logps of the tokens under the policy, the one that drew them, and
     the reference; advantages[R, T] per token, or [R] or [R, 1] per sequence; mask[R, T] the tokens that count (None: all).  reduction "token":
     all of these weigh the same; "sequence": every row that has any does.  `norm` replaces their number where a step comes in several calls."""
+    if stream is None:
+        result = _model_calls.policy_loss(logps, old_logps, advantages, mask, ref_logps, clip_low, clip_high, kl_weight, REDUCTIONS.get(reduction), norm)                        # None: not one of the usual calls
+        if result is not None:
+            return PolicyLoss._make(_native(result, "ef21_policy_loss"))
     dtype = _type_of(logps, "logps")
     if logps.dim() != 2:
         raise ValueError(f"logps must be [rows, length], not {tuple(logps.shape)}")
@@ -702,6 +759,10 @@ def balance_loss(logits: torch.Tensor, choices: torch.Tensor, mask: Optional[tor
                  stream: Optional[torch.cuda.Stream] = None) -> BalanceLoss:
     """Balance loss of a router, tokens per expert, and the gradient of the router's logits[R, E]: choices[R, K] are the experts that each token goes to
     (one outside [0, E) counts for none), mask[R] the tokens that count (None: all)."""
+    if stream is None:
+        result = _model_calls.balance_loss(logits, choices, mask, weight)                        # None: not one of the usual calls
+        if result is not None:
+            return BalanceLoss._make(_native(result, "ef21_balance_loss"))
     dtype, index = _type_of(logits, "logits"), _index_type_of(choices, "choices")
     if logits.dim() != 2:
         raise ValueError(f"logits must be [rows, experts], not {tuple(logits.shape)}")
@@ -732,6 +793,10 @@ def balance_loss(logits: torch.Tensor, choices: torch.Tensor, mask: Optional[tor
 
 def embedding(weight: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """scale * weight[tokens] -> [*tokens.shape, dim]; a token outside the table reads as zeros (as where a table is split by rows)."""
+    if stream is None:
+        result = _model_calls.embedding(weight, tokens, scale)                        # None: not one of the usual calls
+        if result is not None:
+            return _native(result, "ef21_embedding")
     dtype, index = _type_of(weight, "weight"), _index_type_of(tokens, "tokens")
     if weight.dim() != 2:
         raise ValueError(f"weight must be [vocab, dim], not {tuple(weight.shape)}")
@@ -753,6 +818,10 @@ def embedding_grad(grad: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: 
     """The table's gradient [vocab, dim] from that of embedding(): for every token scale times the sum of grad[...] at its positions, in a fixed order.
 
     The result is of grad's type, or float32 (dtype=torch.float32, or an fp32 out).  accumulate adds to out; the token `padding` adds nothing."""
+    if stream is None and out is None and not accumulate:
+        result = _model_calls.embedding_grad(grad, tokens, vocab, scale, padding, dtype)                        # None: not one of the usual calls
+        if result is not None:
+            return _native(result, "ef21_embedding_grad")
     code, index = _type_of(grad, "grad"), _index_type_of(tokens, "tokens")
     if grad.dim() < 1 or tuple(grad.shape[:-1]) != tuple(tokens.shape):
         raise ValueError(f"grad must be of shape {(*tokens.shape, 'dim')}, not {tuple(grad.shape)}")

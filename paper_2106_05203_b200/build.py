@@ -1,5 +1,5 @@
-"""Builds libef21.so (sm_100a, nvcc) and the Python call of its standalone Top-k (_topk_call.so, the C++ compiler, against
-torch's headers) next to this file.  No GPU is needed to build."""
+"""Builds libef21.so (sm_100a, nvcc) and the Python calls that have a native form (_topk_call.so: the standalone Top-k, _model_call.so: the calls of a
+language model's worker; the C++ compiler, against torch's headers) next to this file.  No GPU is needed to build."""
 from __future__ import annotations
 
 import glob
@@ -13,6 +13,9 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libef21.so")
 CALL = os.path.join(HERE, "_topk_call.so")
 CALL_SOURCE = os.path.join(CSRC, "topk_call.cpp")
+MODEL_CALL = os.path.join(HERE, "_model_call.so")
+MODEL_CALL_SOURCE = os.path.join(CSRC, "model_call.cpp")
+HEADER = os.path.join(HERE, "..", "include", "ef21.h")
 
 
 def nvcc_path() -> str:
@@ -27,44 +30,53 @@ def sources():
 
 
 def _newest_source_mtime() -> float:
-    files = [f for f in glob.glob(os.path.join(CSRC, "*")) if f != CALL_SOURCE] + [os.path.join(HERE, "..", "include", "ef21.h")]
+    files = [f for f in glob.glob(os.path.join(CSRC, "*")) if not f.endswith(".cpp")] + [HEADER]
     return max(os.path.getmtime(f) for f in files)
 
 
 def call_built_for() -> str:
-    """What _topk_call.so depends on beside its source; the module carries it as `built_for`."""
+    """What the native calls depend on beside their sources; the modules carry it as `built_for`."""
     import sysconfig
     import torch
     return f"torch {torch.__version__}, {sysconfig.get_config_var('SOABI')}"
 
 
-def _call_is_current() -> bool:
-    if not os.path.exists(CALL) or os.path.getmtime(CALL) < os.path.getmtime(CALL_SOURCE):
+def _is_current(path: str, *sources: str) -> bool:
+    if not os.path.exists(path) or os.path.getmtime(path) < max(os.path.getmtime(f) for f in sources):
         return False
-    with open(CALL, "rb") as f:
+    with open(path, "rb") as f:
         return call_built_for().encode() + b"\0" in f.read()
 
 
-def build_call(force: bool = False) -> str:
-    if not force and _call_is_current():
-        return CALL
+def _build_module(path: str, source: str) -> str:
     import sysconfig
     import torch
     from torch.utils import cpp_extension
     cuda = os.path.join(os.path.dirname(os.path.dirname(nvcc_path())), "include")
     include = [sysconfig.get_paths()["include"], *cpp_extension.include_paths(), cuda]
-    tmp = CALL + f".tmp{os.getpid()}"
+    tmp = path + f".tmp{os.getpid()}"
     subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", f'-DEF21_BUILT_FOR="{call_built_for()}"',
-                    f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *(f"-I{i}" for i in include), CALL_SOURCE,
+                    f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *(f"-I{i}" for i in include), source,
                     *(f"-L{p}" for p in cpp_extension.library_paths()), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda",
                     "-o", tmp], check=True)         # (found by name at run time: the import of torch has loaded them)
-    os.replace(tmp, CALL)
-    return CALL
+    os.replace(tmp, path)
+    return path
+
+
+def build_call(force: bool = False) -> str:
+    """The native call of topk()."""
+    return CALL if not force and _is_current(CALL, CALL_SOURCE) else _build_module(CALL, CALL_SOURCE)
+
+
+def build_model_call(force: bool = False) -> str:
+    """The native calls of a language model's worker (their argument lists are the header's)."""
+    return MODEL_CALL if not force and _is_current(MODEL_CALL, MODEL_CALL_SOURCE, HEADER) else _build_module(MODEL_CALL, MODEL_CALL_SOURCE)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Builds both; returns the path of the library."""
+    """Builds all; returns the path of the library."""
     build_call(force)
+    build_model_call(force)
     return build_library(force, verbose)
 
 

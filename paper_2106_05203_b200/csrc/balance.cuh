@@ -16,7 +16,7 @@ namespace ef21 {
 
 constexpr int BL_THREADS = 256, BL_COUNT_THREADS = 1024;
 constexpr int BL_MAX_EXPERTS = 1024;
-constexpr int BL_MAX_BLOCKS = 148 * 4;
+constexpr int BL_MAX_BLOCKS = 148 * 3;         // (registers for three blocks an SM)
 constexpr int BL_FINISH_COLUMNS = 8, BL_FINISH_GROUPS = 128;
 constexpr unsigned BL_CLUSTER = 8;
 constexpr i64 BL_ONE_CHOICES = 16384, BL_ONE_LOGITS = 32768;      // up to here: one cluster
@@ -80,9 +80,9 @@ __global__ void __launch_bounds__(BL_COUNT_THREADS) balance_count_kernel(const v
 
 // A team of s.lanes lanes takes ROWS rows at a time; lane l has PER vectors of VEC columns, lanes side by side -- of whole vectors where the number of columns
 // is a multiple of them, however the rows are aligned: the order of the additions goes by the number of columns alone.
-// LANES: 32, or 0 where s.lanes may be fewer.
+// LANES: 32 or 16, or 0 where s.lanes may be fewer.
 template <typename T, int VEC, int PER, int ROWS, int LANES>
-__global__ void __launch_bounds__(BL_THREADS) balance_kernel(const T* logits, const void* choices, const unsigned char* mask, int* counts, const BalanceWork* work, T* grad, float* partial,
+__global__ void __launch_bounds__(BL_THREADS, PER * VEC <= 16 ? 3 : 1) balance_kernel(const T* logits, const void* choices, const unsigned char* mask, int* counts, const BalanceWork* work, T* grad, float* partial,
                                                              float* probs, float* loss, BalanceShape s) {
     pdl_wait(logits, choices, mask, counts, work, grad, partial, probs, loss);
     pdl_trigger();
@@ -104,60 +104,75 @@ __global__ void __launch_bounds__(BL_THREADS) balance_kernel(const T* logits, co
     }
     const double N = (double)(s.one ? seen : work->tokens), KN = N * s.chosen;
     auto column_of = [&](int i) { return (lane + i / VEC * lanes) * VEC + i % VEC; };
-    float apart[PER * VEC], sum[PER * VEC];
+    constexpr int PAIRS = VEC > 1 ? PER * VEC / 2 : PER;
+    __shared__ float about_mean[BL_MAX_EXPERTS];
+    for (int e = tid; e < E; e += BL_THREADS) about_mean[e] = N > 0.0 ? (float)(((double)(s.one ? here[e] : counts[e]) * E - KN) / (KN * E)) : 0.f;
+    __syncthreads();
+    auto share = [&](int e) { return e < E ? about_mean[e] : 0.f; };
+    Two apart[PAIRS], sum[PAIRS];
 #pragma unroll
-    for (int i = 0; i < PER * VEC; ++i) {
-        const int e = column_of(i);
-        apart[i] = e < E && N > 0.0 ? (float)(((double)(s.one ? here[e] : counts[e]) * E - KN) / (KN * E)) : 0.f;
-        sum[i] = 0.f;
+    for (int i = 0; i < PAIRS; ++i) {
+        apart[i] = VEC > 1 ? two(share(column_of(2 * i)), share(column_of(2 * i + 1))) : two(share(column_of(i)), 0.f);
+        sum[i] = two(0.f);
     }
     const float factor = N > 0.0 ? (float)(s.weight * E / N) : 0.f;
     const i64 step = (i64)gridDim.x * groups;
-    for (i64 row0 = (i64)blockIdx.x * groups + group; row0 - group < s.rows; row0 += step * ROWS) {     // (whole warps: the shuffles need every lane)
-        float f[ROWS][PER * VEC], top[ROWS], total[ROWS], mean[ROWS];
-        bool keep[ROWS];
-        uint4 raw[ROWS][VEC > 1 ? PER : 1];
+    uint4 raw[ROWS][VEC > 1 ? PER : 1];
+    float single[ROWS][VEC > 1 ? 1 : PER];
+    bool counts_in[ROWS];
+    auto fetch = [&](i64 row0) {
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             const i64 row = row0 + r * step;
-            keep[r] = row < s.rows && (!mask || mask[row]);
+            counts_in[r] = row < s.rows && (!mask || mask[row]);
             const T* x = logits + row * s.logit_stride;
-            if constexpr (VEC > 1) {
 #pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    const int at = (lane + i * lanes) * VEC;
-                    if (row >= s.rows || at >= E) continue;
-                    if (s.whole_in) { raw[r][i] = load_once(x + at); continue; }
+            for (int i = 0; i < PER; ++i) {
+                const int at = (lane + i * lanes) * VEC;
+                if (row >= s.rows || at >= E) continue;
+                if constexpr (VEC == 1) {
+                    single[r][i] = Elem<T>::get(x[at]);
+                } else if (s.whole_in) {
+                    raw[r][i] = load_once(x + at);
+                } else {
                     float v[VEC];
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) v[e] = Elem<T>::get(x[at + e]);
                     raw[r][i] = Elem<T>::pack(v);
                 }
-            } else {
-#pragma unroll
-                for (int i = 0; i < PER; ++i) f[r][i] = row < s.rows && column_of(i) < E ? Elem<T>::get(x[column_of(i)]) : -INFINITY;
             }
         }
+    };
+    fetch((i64)blockIdx.x * groups + group);
+    for (i64 row0 = (i64)blockIdx.x * groups + group; row0 - group < s.rows; row0 += step * ROWS) {     // (whole warps: the shuffles need every lane)
+        // (fp32 pairs: one instruction for two columns; a single column has a pair to itself)
+        Two f[ROWS][PAIRS];
+        float top[ROWS], total[ROWS], mean[ROWS];
+        bool keep[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) keep[r] = counts_in[r];
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             top[r] = -INFINITY;
-            if constexpr (VEC > 1) {
 #pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    constexpr unsigned none = Elem<T>::NEG_INF;
-                    if (!keep[r] || (lane + i * lanes) * VEC >= E) raw[r][i] = make_uint4(none, none, none, none);
+            for (int i = 0; i < PER; ++i) {
+                const bool none = !keep[r] || (lane + i * lanes) * VEC >= E;
+                if constexpr (VEC == 1) {
+                    if (none) single[r][i] = -INFINITY;
+                    top[r] = fmaxf(top[r], single[r][i]);
+                    f[r][i] = two(single[r][i], -INFINITY);
+                } else {
+                    constexpr unsigned nothing = Elem<T>::NEG_INF;
+                    if (none) raw[r][i] = make_uint4(nothing, nothing, nothing, nothing);
+                    top[r] = fmaxf(top[r], Elem<T>::top(raw[r][i]));
                     float v[VEC];
                     Elem<T>::unpack(raw[r][i], v);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) f[r][i * VEC + e] = v[e];
+                    for (int e = 0; e < VEC; e += 2) f[r][(i * VEC + e) / 2] = two(v[e], v[(e + 1) % VEC]);
                 }
-            } else if (!keep[r]) {
-#pragma unroll
-                for (int i = 0; i < PER; ++i) f[r][i] = -INFINITY;
             }
-#pragma unroll
-            for (int i = 0; i < PER * VEC; ++i) top[r] = fmaxf(top[r], f[r][i]);
         }
+        fetch(row0 + step * ROWS);                                           // (on their way while these rows are worked on)
 #pragma unroll
         for (int o = lanes >> 1; o > 0; o >>= 1) {
 #pragma unroll
@@ -165,14 +180,26 @@ __global__ void __launch_bounds__(BL_THREADS) balance_kernel(const T* logits, co
         }
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-            const float base = top[r] == -INFINITY ? 0.f : top[r];           // (a row of -inf only, or left out: all 0)
-            total[r] = 0.f; mean[r] = 0.f;
+            float base = top[r] == -INFINITY ? 0.f : top[r];                 // (a row of -inf only, or left out: all 0)
+            const Two exponent = two(LOG2E);
+            if (base < -1e38f) {                                             // (a mask of the type's lowest value: it times log2 e would overflow)
 #pragma unroll
-            for (int i = 0; i < PER * VEC; ++i) {
-                f[r][i] = exp2_fast((f[r][i] - base) * LOG2E);
-                total[r] += f[r][i];
-                mean[r] = fmaf(f[r][i], apart[i], mean[r]);
+                for (int i = 0; i < PAIRS; ++i) f[r][i] = add2(f[r][i], two(-base));
+                base = 0.f;
             }
+            const Two shift = two(-base * LOG2E);
+            Two sum2 = two(0.f), mean2 = two(0.f);
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {
+                float a, b;
+                split(fma2(f[r][i], exponent, shift), a, b);
+                f[r][i] = two(exp2_fast(a), exp2_fast(b));
+                sum2 = add2(sum2, f[r][i]);
+                mean2 = fma2(f[r][i], apart[i], mean2);
+            }
+            float a, b;
+            split(sum2, a, b); total[r] = a + b;
+            split(mean2, a, b); mean[r] = a + b;
         }
 #pragma unroll
         for (int o = lanes >> 1; o > 0; o >>= 1) {
@@ -186,42 +213,46 @@ __global__ void __launch_bounds__(BL_THREADS) balance_kernel(const T* logits, co
         for (int r = 0; r < ROWS; ++r) {
             const i64 row = row0 + r * step;
             if (row >= s.rows) continue;
-            const float scale = total[r] == 0.f ? 0.f : 1.f / total[r], about = mean[r] * scale, slope = factor * scale;
+            const float scale = total[r] == 0.f ? 0.f : __fdividef(1.f, total[r]), slope = factor * scale;
+            const Two p = two(scale), m = two(slope), about = two(-mean[r] * scale * slope);
 #pragma unroll
-            for (int i = 0; i < PER * VEC; ++i) {
-                sum[i] = fmaf(f[r][i], scale, sum[i]);
-                f[r][i] = f[r][i] * slope * (apart[i] - about);
+            for (int i = 0; i < PAIRS; ++i) {
+                sum[i] = fma2(f[r][i], p, sum[i]);
+                f[r][i] = mul2(f[r][i], fma2(apart[i], m, about));
             }
             T* g = grad + row * E;
-            if constexpr (VEC > 1) {
 #pragma unroll
-                for (int i = 0; i < PER; ++i) {
+            for (int i = 0; i < PER; ++i) {
+                const int at = (lane + i * lanes) * VEC;
+                if (at >= E) continue;
+                if constexpr (VEC == 1) {
+                    float a, b;
+                    split(f[r][i], a, b);
+                    g[at] = Elem<T>::put(a);
+                } else {
                     float v[VEC];
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) v[e] = f[r][i * VEC + e];
-                    const int at = (lane + i * lanes) * VEC;
-                    if (at >= E) continue;
+                    for (int e = 0; e < VEC; e += 2) split(f[r][(i * VEC + e) / 2], v[e], v[(e + 1) % VEC]);
                     if (s.whole_out) { store_vec(g + at, Elem<T>::pack(v)); continue; }
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) g[at + e] = Elem<T>::put(v[e]);
                 }
-            } else {
-#pragma unroll
-                for (int i = 0; i < PER; ++i) if (column_of(i) < E) g[column_of(i)] = Elem<T>::put(f[r][i]);
             }
         }
     }
     // column sums: a warp's teams by shuffles, then the block's warps one after the other
     for (int o = lanes; o < 32; o <<= 1) {
 #pragma unroll
-        for (int i = 0; i < PER * VEC; ++i) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
+        for (int i = 0; i < PAIRS; ++i) sum[i] = add2(sum[i], __shfl_xor_sync(0xffffffffu, sum[i], o));
     }
     for (int w = 0; w < BL_THREADS / 32; ++w) {
         if (tid >> 5 == w && (tid & 31) < lanes) {
+            auto add = [&](int e, float v) { if (e < E) column[e] = w == 0 ? v : column[e] + v; };
 #pragma unroll
-            for (int i = 0; i < PER * VEC; ++i) {
-                const int e = column_of(i);
-                if (e < E) column[e] = w == 0 ? sum[i] : column[e] + sum[i];
+            for (int i = 0; i < PAIRS; ++i) {
+                float a, b;
+                split(sum[i], a, b);
+                if (VEC > 1) { add(column_of(2 * i), a); add(column_of(2 * i + 1), b); } else add(column_of(i), a);
             }
         }
         __syncthreads();

@@ -94,12 +94,44 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return y;
 }
 
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+// e^x to a few units in the last place: what the product with log2 e loses is put back to first order.  (Below 2^-126: 0.)
+__device__ __forceinline__ float exp_fast(float x) {
+    const float t = x * LOG2E, y = exp2_fast(t), lost = fmaf(x, LOG2E, -t);
+    return fabsf(lost) <= 1.f ? fmaf(y, lost * LN2, y) : y;              // (infinite t: nothing to put back)
+}
+
+// Two fp32 values, and one instruction for both.
+typedef unsigned long long Two;
+__device__ __forceinline__ Two two(float a, float b) {
+    Two r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ Two two(float a) { return two(a, a); }
+__device__ __forceinline__ void split(Two v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ Two mul2(Two a, Two b) {
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ Two add2(Two a, Two b) {
+    Two r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 // Elements in front of the first 16-byte boundary of a row.
 template <typename T>
 __device__ __forceinline__ int row_head(const T* row) {
     return (int)(((16u - (unsigned)(reinterpret_cast<uintptr_t>(row) & 15u)) & 15u) / sizeof(T));
 }
 
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 }  // namespace ef21

@@ -86,7 +86,7 @@ struct PolicyWork { int* tokens; i64* counted; PolicySums* partial; };
 size_t policy_layout(void* p, i64 rows, PolicyWork& w) {
     Sections s(p);
     w.tokens = s.take<int>((size_t)rows);
-    w.counted = s.take<i64>(PO_MAX_BLOCKS);
+    w.counted = s.take<i64>(PO_COUNT_BLOCKS);
     w.partial = s.take<PolicySums>(PO_MAX_BLOCKS);
     return s.used;
 }
@@ -263,7 +263,7 @@ ef21_status ef21_policy_loss(const void* logps_dev, const void* old_dev, const v
     policy_layout(workspace_dev, rows, w);
     cudaStream_t st = stream_of(cuda_stream);
     const bool by_sequence = reduction == EF21_REDUCE_SEQUENCES, count = mask_dev && (norm == 0.0 || by_sequence);
-    const unsigned count_blocks = grid_of(rows, PO_THREADS / 32, PO_MAX_BLOCKS);
+    const unsigned count_blocks = grid_of(rows, PO_COUNT_THREADS / 32, PO_COUNT_BLOCKS);
     const i64 all = rows * length;
     auto whole = [&](const void* p, i64 stride) { return aligned(p, 16) && (!p || rows <= 1 || stride == length); };
     const int vec = 16 / bytes_of(dtype);
@@ -271,15 +271,17 @@ ef21_status ef21_policy_loss(const void* logps_dev, const void* old_dev, const v
                       aligned(grad_out_dev, 16) && aligned(mask_dev, vec) && (!mask_dev || rows <= 1 || mask_stride == length);
     // one cluster: its blocks count all tokens themselves, words of 4 or 8 where the arrays are flat, else one by one
     const bool one = rows <= PO_ONE_ROWS && all <= (flat ? PO_ONE_TOKENS : PO_ONE_TOKENS / 8);
-    if (count && !one) CU(launch(policy_count_kernel, count_blocks, PO_THREADS, 0, st, 1, mask_dev, w.tokens, w.counted, rows, length, mask_stride, (int)by_sequence));
+    if (count && !one) CU(launch(policy_count_kernel, count_blocks, PO_COUNT_THREADS, 0, st, 1, mask_dev, w.tokens, w.counted, rows, length, mask_stride, (int)by_sequence));
     return by_dtype(dtype, [&](auto* type) -> ef21_status {
         typedef typename Pointee<decltype(type)>::type T;
         constexpr int VEC = Elem<T>::VEC;
         const T *logps = static_cast<const T*>(logps_dev), *old = static_cast<const T*>(old_dev), *ref = static_cast<const T*>(ref_dev), *adv = static_cast<const T*>(advantages_dev);
         T* grad = static_cast<T*>(grad_out_dev);
+        const i64 items = flat ? all / VEC : all, most = one ? PO_CLUSTER : PO_MAX_BLOCKS;
+        const i64 per_block = PO_THREADS * (one ? ceil_div(items, PO_THREADS * most) : ceil_div(items, PO_THREADS * PO_VECTORS * most) * PO_VECTORS);
+        const unsigned blocks = grid_of(items, per_block > 0 ? per_block : 1, most);
         const PolicyShape s{rows, length, logps_stride, old_stride, ref_stride, mask_stride, advantages_stride, advantages_per_token, by_sequence,
-                            std::log1p(-clip_low), std::log1p(clip_high), (float)(1e-6 * (1.0 - std::log1p(-clip_low))), (float)(1e-6 * (1.0 + std::log1p(clip_high))), (float)(1.0 - clip_low), (float)(1.0 + clip_high), (float)kl_weight, norm, (int)count_blocks, (int)one};
-        const unsigned blocks = grid_of(all, (i64)PO_THREADS * (flat ? VEC : 1), one ? PO_CLUSTER : PO_MAX_BLOCKS);
+                            std::log1p(-clip_low), std::log1p(clip_high), (float)(1e-6 * (1.0 + std::fmax(-std::log1p(-clip_low), std::log1p(clip_high)))), (float)(1.0 - clip_low), (float)(1.0 + clip_high), (float)kl_weight, norm, (int)count_blocks, per_block, (int)one};
         const int* tokens = count && !one ? w.tokens : nullptr;
         const i64* counted = count && !one ? w.counted : nullptr;
         if (flat) CU(launch(policy_kernel<T, true>, blocks, PO_THREADS, 0, st, one ? blocks : 1, logps, old, ref, adv, mask_dev, tokens, counted, grad, w.partial, terms_out_dev, s));
@@ -313,7 +315,8 @@ ef21_status ef21_balance_loss(const void* logits_dev, int32_t dtype, int64_t row
         const bool vectors = experts % V == 0;
         const i64 columns = vectors ? experts / V : experts;
         BalanceShape s{rows, (int)experts, (int)chosen, index_type, logits_stride, choices_stride, weight, 1, 0, aligned(logits, 16) && logits_stride % V == 0, aligned(grad, 16)};
-        while (s.lanes < 32 && s.lanes < columns) s.lanes *= 2;
+        // two vectors a lane where there are enough: a row's shuffles, division and addresses are shared by fewer lanes
+        while (s.lanes < 32 && s.lanes * (vectors ? 2 : 1) < columns) s.lanes *= 2;
         s.one = rows * chosen <= BL_ONE_CHOICES && rows * experts <= BL_ONE_LOGITS;
         const unsigned blocks = grid_of(rows, BL_THREADS / s.lanes, s.one ? BL_CLUSTER : BL_MAX_BLOCKS);
         if (!s.one) {
@@ -324,11 +327,10 @@ ef21_status ef21_balance_loss(const void* logits_dev, int32_t dtype, int64_t row
             CU(launch(kernel, blocks, BL_THREADS, 0, st, s.one ? blocks : 1, logits, choices_dev, mask_dev, counts_out_dev, w.work, grad, w.partial, probs_out_dev, loss_out_dev, s));
             return EF21_OK;
         };
-        // rows in flight per team: 16 to 32 values per lane
+        // rows in flight per team: 16 values per lane or more
         const bool full = s.lanes == 32;
         if (vectors) {
-            if (columns <= 32) EF(full ? run(balance_kernel<T, V, 1, 16 / V, 32>) : run(balance_kernel<T, V, 1, 16 / V, 0>));
-            else if (columns <= 64) EF(run(balance_kernel<T, V, 2, 1, 32>));
+            if (columns <= 64) EF(full ? run(balance_kernel<T, V, 2, 8 / V, 32>) : s.lanes == 16 ? run(balance_kernel<T, V, 2, 8 / V, 16>) : run(balance_kernel<T, V, 2, 8 / V, 0>));
             else if (columns <= 128) EF(run(balance_kernel<T, V, 4, 1, 32>));
             else if constexpr (V == 4) EF(run(balance_kernel<T, V, 8, 1, 32>));
         } else {

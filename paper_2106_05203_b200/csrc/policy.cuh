@@ -14,8 +14,10 @@
 
 namespace ef21 {
 
-constexpr int PO_THREADS = 256;
-constexpr int PO_MAX_BLOCKS = 148 * 8;
+constexpr int PO_THREADS = 128;              // small blocks: where a mask leaves runs of tokens out, blocks differ in their work
+constexpr int PO_VECTORS = 8;                // per thread, more where there would be more than PO_MAX_BLOCKS blocks
+constexpr int PO_MAX_BLOCKS = 8192;
+constexpr int PO_COUNT_THREADS = 256, PO_COUNT_BLOCKS = 128;
 constexpr int PO_FINISH_THREADS = 1024;
 constexpr i64 PO_ONE_TOKENS = 16384;         // up to here (and PO_ONE_ROWS rows): one cluster of up to eight blocks
 constexpr int PO_ONE_ROWS = 1024;
@@ -27,17 +29,17 @@ struct PolicyShape {
     int adv_per_token;
     int by_sequence;
     double log_low, log_high;                // log(1 - lo), log(1 + hi)
-    float near_low, near_high;               // how close to these a difference in 32 bits says nothing
+    float near;                              // how close to these a difference in 32 bits says nothing
     float low, high;                         // 1 - lo, 1 + hi
     float kl_weight;
     double norm;                             // 0: counted
     int count_blocks;
+    i64 per_block;                           // vectors (flat) or tokens of a block
     int one;                                 // all blocks are one cluster: they count, and write the terms
 };
 
-// exp(x) - 1 - x >= 0, to a few units in the last place: the series about 0, where the difference would lose everything.
+// exp(x) - 1 - x >= 0, to a few units in the last place, for |x| <= 1: the series about 0, where the difference would lose everything.
 __device__ __forceinline__ float exp_minus_line(float x) {
-    if (fabsf(x) > 1.f) return expf(x) - 1.f - x;
     float p = 1.f / 39916800.f;                                          // 1 / 11!
     p = fmaf(p, x, 1.f / 3628800.f); p = fmaf(p, x, 1.f / 362880.f); p = fmaf(p, x, 1.f / 40320.f); p = fmaf(p, x, 1.f / 5040.f);
     p = fmaf(p, x, 1.f / 720.f); p = fmaf(p, x, 1.f / 120.f); p = fmaf(p, x, 1.f / 24.f); p = fmaf(p, x, 1.f / 6.f); p = fmaf(p, x, 0.5f);
@@ -49,13 +51,13 @@ __device__ __forceinline__ int count_bytes(unsigned w) { return __popc(__vcmpne4
 __device__ __forceinline__ int count_bytes(unsigned long long w) { return count_bytes((unsigned)w) + count_bytes((unsigned)(w >> 32)); }
 
 // Tokens of every row, and per block how many tokens (by_sequence: rows that have any) its rows hold.
-__global__ void __launch_bounds__(PO_THREADS) policy_count_kernel(const unsigned char* mask, int* tokens, i64* partial, i64 rows, i64 length, i64 stride, int by_sequence) {
+__global__ void __launch_bounds__(PO_COUNT_THREADS) policy_count_kernel(const unsigned char* mask, int* tokens, i64* partial, i64 rows, i64 length, i64 stride, int by_sequence) {
     pdl_wait(mask, tokens, partial);
     pdl_trigger();
-    __shared__ i64 scratch[PO_THREADS / 32];
+    __shared__ i64 scratch[PO_COUNT_THREADS / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     i64 mine = 0;
-    for (i64 r = (i64)blockIdx.x * (PO_THREADS / 32) + warp; r < rows; r += (i64)gridDim.x * (PO_THREADS / 32)) {
+    for (i64 r = (i64)blockIdx.x * (PO_COUNT_THREADS / 32) + warp; r < rows; r += (i64)gridDim.x * (PO_COUNT_THREADS / 32)) {
         const unsigned char* m = mask + r * stride;
         const int head = (int)min((i64)row_head(m), length);
         const i64 vectors = (length - head) / 16, tail = head + vectors * 16;
@@ -77,7 +79,7 @@ __global__ void __launch_bounds__(PO_THREADS) policy_count_kernel(const unsigned
     __syncthreads();
     if (threadIdx.x == 0) {
         i64 sum = 0;
-        for (int w = 0; w < PO_THREADS / 32; ++w) sum += scratch[w];
+        for (int w = 0; w < PO_COUNT_THREADS / 32; ++w) sum += scratch[w];
         partial[blockIdx.x] = sum;
     }
 }
@@ -89,29 +91,61 @@ __device__ __forceinline__ void write_terms(float* terms, double pg, double kl, 
     terms[1] = (float)pg; terms[2] = (float)kl; terms[3] = (float)clipped;
 }
 
-// One token: its terms without their weight are added to pg, kl and clip, its gradient (without the weight) returned.
-__device__ __forceinline__ float policy_token(float lp, float old, float ref, bool has_ref, float A, const PolicyShape& s, float& pg, float& kl, float& clip) {
-    const float d = lp - old;
-    // beyond the border that counts for the sign of A?  The fp32 difference is good to half a step of its own; next to the border the exact one is taken
-    const bool up = A > 0.f;
-    const double border = up ? s.log_high : s.log_low;
-    const float past = d - (float)border;
-    bool clipped = up ? past > 0.f : past < 0.f;
-    if (fabsf(past) <= (up ? s.near_high : s.near_low)) {
-        const double exact = (double)lp - (double)old;
-        clipped = up ? exact > border : exact < border;
+// N tokens, ALL or those whose byte of the mask word is not 0: their terms without their weight are added to pg, kl and clip, g is their gradient
+// (without the weight; 0 for the others).  No branch but two rare ones: lanes differ.
+template <int N, bool ALL, typename Word>
+__device__ __forceinline__ void policy_tokens(const float (&lp)[N], const float (&old)[N], const float (&ref)[N], bool has_ref, const float (&A)[N], Word w, const PolicyShape& s,
+                                              float (&g)[N], float& pg, float& kl, float& clip) {
+    // past the border that counts for the sign of A?  The fp32 difference is good to half a step of its own; next to a border the exact one is taken
+    bool cut[N];
+    float closest = INFINITY;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const float past = (lp[e] - old[e]) - (A[e] > 0.f ? (float)s.log_high : (float)s.log_low);
+        closest = fminf(closest, fabsf(past));
+        cut[e] = past * A[e] > 0.f;
     }
-    clipped = clipped && A != 0.f;
-    const float r = clipped ? (up ? s.high : s.low) : A == 0.f ? 0.f : expf(d), gain = r * A;
-    float g = clipped ? 0.f : -gain;
-    pg -= gain;
-    clip += clipped ? 1.f : 0.f;
+    if (closest <= s.near) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const double exact = (double)lp[e] - (double)old[e];
+            cut[e] = A[e] > 0.f ? exact > s.log_high : A[e] < 0.f && exact < s.log_low;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const bool in = ALL || (w >> (8 * e) & 255u) != 0;
+        const float r = cut[e] ? (A[e] > 0.f ? s.high : s.low) : A[e] == 0.f ? 0.f : exp_fast(lp[e] - old[e]), gain = r * A[e];
+        pg -= in ? gain : 0.f;
+        clip += in && cut[e] ? 1.f : 0.f;
+        g[e] = cut[e] ? 0.f : -gain;
+    }
     if (has_ref) {
-        const float delta = ref - lp, k = exp_minus_line(delta);
-        kl += k;
-        g -= s.kl_weight * (k + delta);
+        float k[N], farthest = 0.f;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float delta = ref[e] - lp[e];
+            farthest = delta != delta ? INFINITY : fmaxf(farthest, fabsf(delta));
+            k[e] = exp_minus_line(delta);
+        }
+        if (!(farthest <= 1.f)) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float delta = ref[e] - lp[e];
+                if (!(fabsf(delta) <= 1.f)) k[e] = expf(delta) - 1.f - delta;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const bool in = ALL || (w >> (8 * e) & 255u) != 0;
+            kl += in ? k[e] : 0.f;
+            g[e] -= s.kl_weight * (k[e] + (ref[e] - lp[e]));
+        }
     }
-    return g;
+    if (!ALL) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) if ((w >> (8 * e) & 255u) == 0) g[e] = 0.f;
+    }
 }
 
 // FLAT: all arrays are contiguous, a vector of VEC tokens may run over the end of a row.  Otherwise token by token, any strides.
@@ -122,7 +156,6 @@ __global__ void __launch_bounds__(PO_THREADS) policy_kernel(const T* logps, cons
     pdl_trigger();
     constexpr int VEC = FLAT ? Elem<T>::VEC : 1;
     typedef typename MaskWord<Elem<T>::VEC>::type Word;
-    __shared__ double scratch[PO_THREADS / 32];
     __shared__ int row_tokens[PO_ONE_ROWS], seen;
     const int tid = threadIdx.x;
     const bool in_block = s.one && mask && (s.norm == 0.0 || s.by_sequence);
@@ -164,10 +197,13 @@ __global__ void __launch_bounds__(PO_THREADS) policy_kernel(const T* logps, cons
     if (norm == 0.0) {
         if (in_block) {
             norm = (double)seen;
-        } else if (counted) {
-            double n = 0.0;
-            for (int b = tid; b < s.count_blocks; b += PO_THREADS) n += (double)counted[b];
-            norm = block_sum<PO_THREADS>(n, scratch);
+        } else if (counted) {                                          // every warp for itself: whole numbers
+            i64 n = 0;
+#pragma unroll
+            for (int b = 0; b < PO_COUNT_BLOCKS; b += 32) n += b + (tid & 31) < s.count_blocks ? counted[b + (tid & 31)] : 0;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
+            norm = (double)n;
         } else {
             norm = s.by_sequence ? (s.length > 0 ? (double)s.rows : 0.0) : (double)s.rows * (double)s.length;
         }
@@ -179,7 +215,7 @@ __global__ void __launch_bounds__(PO_THREADS) policy_kernel(const T* logps, cons
         return n > 0 ? __fdividef(inverse, (float)n) : 0.f;
     };
     PolicySums sums;
-    const i64 all = s.rows * s.length, vectors = all / VEC, step = (i64)gridDim.x * PO_THREADS;
+    const i64 all = s.rows * s.length, vectors = all / VEC, step = PO_THREADS;
     const bool small = all < (1ll << 31);                              // (a division of 32 bits)
     auto token = [&](i64 i) {                                       // one token, any strides
         const i64 row = small ? (i64)((unsigned)i / (unsigned)s.length) : i / s.length, t = i - row * s.length;
@@ -187,21 +223,23 @@ __global__ void __launch_bounds__(PO_THREADS) policy_kernel(const T* logps, cons
         if (mask && !mask[row * s.mask_stride + t]) { *g = Elem<T>::put(0.f); return; }
         float pg = 0.f, kl = 0.f, clip = 0.f;
         const float A = Elem<T>::get(adv[row * s.adv_stride + (s.adv_per_token ? t : 0)]), weighs = weight(row);
-        const float v = policy_token(Elem<T>::get(logps[row * s.logp_stride + t]), Elem<T>::get(old[row * s.old_stride + t]),
-                                     ref ? Elem<T>::get(ref[row * s.ref_stride + t]) : 0.f, ref != nullptr, A, s, pg, kl, clip);
-        *g = Elem<T>::put(weighs * v);
+        const float x[1] = {Elem<T>::get(logps[row * s.logp_stride + t])}, o[1] = {Elem<T>::get(old[row * s.old_stride + t])}, a[1] = {A};
+        const float f[1] = {ref ? Elem<T>::get(ref[row * s.ref_stride + t]) : 0.f};
+        float v[1];
+        policy_tokens<1, true, unsigned>(x, o, f, ref != nullptr, a, 1u, s, v, pg, kl, clip);
+        *g = Elem<T>::put(weighs * v[0]);
         sums.pg += (double)(weighs * pg); sums.kl += (double)(weighs * kl); sums.clipped += (double)(weighs * clip);
     };
-    auto word = [&](i64 v) { return !FLAT || v >= vectors ? (Word)0 : mask ? *reinterpret_cast<const Word*>(mask + v * VEC) : ~(Word)0; };
-    const i64 start = (i64)blockIdx.x * PO_THREADS + tid;
+    const i64 start = (i64)blockIdx.x * s.per_block + tid, stop = min(start - tid + s.per_block, vectors);
+    auto word = [&](i64 v) { return !FLAT || v >= stop ? (Word)0 : mask ? *reinterpret_cast<const Word*>(mask + v * VEC) : ~(Word)0; };
     if constexpr (!FLAT) {
-        for (i64 v = start; v < vectors; v += step) token(v);
-    } else if (start < vectors) {
+        for (i64 v = start; v < stop; v += step) token(v);
+    } else if (start < stop) {
         Word next = word(start);
         // row and position of the vector, carried along
         const i64 skip_rows = step * VEC / s.length, skip = step * VEC - skip_rows * s.length;
         i64 row = start * VEC / s.length, t = start * VEC - row * s.length;
-        for (i64 v = start; v < vectors; v += step) {
+        for (i64 v = start; v < stop; v += step) {
             const i64 i = v * VEC;
             const Word w = next;
             next = word(v + step);                                     // (on its way while this one's tokens are)
@@ -211,7 +249,7 @@ __global__ void __launch_bounds__(PO_THREADS) policy_kernel(const T* logps, cons
                 float x[VEC], o[VEC], f[VEC], A[VEC], g[VEC];
                 const uint4 ux = load_once(logps + i), uo = load_once(old + i), uf = ref ? load_once(ref + i) : make_uint4(0u, 0u, 0u, 0u);
                 const uint4 ua = s.adv_per_token ? load_once(adv + i) : make_uint4(0u, 0u, 0u, 0u);
-                float weighs = weight(row);
+                const float weighs = weight(row);
                 Elem<T>::unpack(ux, x); Elem<T>::unpack(uo, o); Elem<T>::unpack(uf, f); Elem<T>::unpack(ua, A);
                 if (!s.adv_per_token) {
                     const float a = Elem<T>::get(adv[row * s.adv_stride]);
@@ -220,24 +258,16 @@ __global__ void __launch_bounds__(PO_THREADS) policy_kernel(const T* logps, cons
                 }
                 float pg = 0.f, kl = 0.f, clip = 0.f;
                 if (t + VEC <= s.length) {
+                    // (a word of ones: all; other bytes may stand for true, they are looked at one by one)
+                    if (!mask || w == (Word)0x0101010101010101ull) policy_tokens<VEC, true, Word>(x, o, f, ref != nullptr, A, w, s, g, pg, kl, clip);
+                    else policy_tokens<VEC, false, Word>(x, o, f, ref != nullptr, A, w, s, g, pg, kl, clip);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) g[e] = (w >> (8 * e) & 255u) != 0 ? weighs * policy_token(x[e], o[e], f[e], ref != nullptr, A[e], s, pg, kl, clip) : 0.f;
+                    for (int e = 0; e < VEC; ++e) g[e] *= weighs;
                 } else {                                               // it runs over the end of a row
-                    i64 at = row, left = s.length - t;
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        if (left == 0) {
-                            sums.pg += (double)(weighs * pg); sums.kl += (double)(weighs * kl); sums.clipped += (double)(weighs * clip);
-                            pg = kl = clip = 0.f;
-                            ++at; left = s.length;
-                            weighs = weight(at);
-                        }
-                        --left;
-                        const float a = s.adv_per_token ? A[e] : Elem<T>::get(adv[at * s.adv_stride]);
-                        g[e] = (w >> (8 * e) & 255u) != 0 ? weighs * policy_token(x[e], o[e], f[e], ref != nullptr, a, s, pg, kl, clip) : 0.f;
-                    }
+#pragma unroll 1
+                    for (int e = 0; e < VEC; ++e) token(i + e);
                 }
-                store_vec(grad + i, Elem<T>::pack(g));
+                if (t + VEC <= s.length) store_vec(grad + i, Elem<T>::pack(g));
                 sums.pg += (double)(weighs * pg); sums.kl += (double)(weighs * kl); sums.clipped += (double)(weighs * clip);
             }
             row += skip_rows; t += skip;
@@ -245,9 +275,14 @@ __global__ void __launch_bounds__(PO_THREADS) policy_kernel(const T* logps, cons
         }
     }
     if (FLAT && blockIdx.x == 0 && vectors * VEC + tid < all) token(vectors * VEC + tid);
-    sums.pg = block_sum<PO_THREADS>(sums.pg, scratch);
-    sums.kl = block_sum<PO_THREADS>(sums.kl, scratch);
-    sums.clipped = block_sum<PO_THREADS>(sums.clipped, scratch);
+    __shared__ PolicySums of_warp[PO_THREADS / 32];
+    sums.pg = warp_sum(sums.pg); sums.kl = warp_sum(sums.kl); sums.clipped = warp_sum(sums.clipped);
+    if ((tid & 31) == 0) of_warp[tid >> 5] = sums;
+    __syncthreads();
+    if (tid == 0) {
+#pragma unroll
+        for (int w = 1; w < PO_THREADS / 32; ++w) { sums.pg += of_warp[w].pg; sums.kl += of_warp[w].kl; sums.clipped += of_warp[w].clipped; }
+    }
     if (s.one) {
         __shared__ double mine[3];
         double all_sums[3] = {sums.pg, sums.kl, sums.clipped};
