@@ -360,10 +360,11 @@ enum {
  * `vocab` logits; row (b, t) starts at b batch_stride + t row_stride, its target is targets[b targets_batch_stride + t].
  * logps_out and lse_out: [batch][length].  scale > 0 (one over a temperature).  A row whose target is `ignore` is not read: 0 and 0.
  * A target outside [0, vocab): NaN and NaN.  A row of -inf only: -inf and -inf.  +inf or NaN among the logits: NaN. */
+size_t ef21_token_logprobs_workspace_bytes(int32_t dtype, int64_t batch, int64_t length, int64_t vocab);
 ef21_status ef21_token_logprobs(const void* logits_dev, int32_t dtype, int64_t batch, int64_t length, int64_t vocab,
                                 int64_t batch_stride, int64_t row_stride, const void* targets_dev, int32_t index_type,
                                 int64_t targets_batch_stride, float scale, int64_t ignore, float* logps_out_dev,
-                                float* lse_out_dev, void* cuda_stream);
+                                float* lse_out_dev, void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
 /* The logits' gradient, given that of the log-probabilities (grad_dev[batch][length]) and the forward pass's lse_dev:
  * out_j = scale grad (1[j = target] - exp(scale x_j - lse)), in the logits' type.  out may be the logits themselves (same strides), or must not
  * overlap them.  Rows that are ignored, whose grad is 0, or whose lse is -inf get zeros and are not read. */

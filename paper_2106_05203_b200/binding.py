@@ -77,7 +77,8 @@ SIGNATURES = {
     "ef21_set_path": (ctypes.c_int, [_vp, _i32]),
     "ef21_last_path": (_i32, [_vp]),
     "ef21_launch_count": (_i64, [_vp]),
-    "ef21_token_logprobs": (ctypes.c_int, [_vp, _i32, _i64, _i64, _i64, _i64, _i64, _vp, _i32, _i64, _f32, _i64, _vp, _vp, _vp]),
+    "ef21_token_logprobs_workspace_bytes": (_sz, [_i32, _i64, _i64, _i64]),
+    "ef21_token_logprobs": (ctypes.c_int, [_vp, _i32, _i64, _i64, _i64, _i64, _i64, _vp, _i32, _i64, _f32, _i64, _vp, _vp, _vp, _sz, _vp]),
     "ef21_token_logprobs_grad": (ctypes.c_int, [_vp, _i32, _i64, _i64, _i64, _i64, _i64, _vp, _i32, _i64, _vp, _vp, _f32, _i64, _vp, _i64, _i64, _vp]),
     "ef21_preference_loss_workspace_bytes": (_sz, [_i64, _i64]),
     "ef21_preference_loss": (ctypes.c_int, [_vp, _vp, _vp, _i32, _i64, _i64, _i64, _i64, _i64, _f64, _f64, _f64, _vp, _vp, _vp, _vp, _sz, _vp]),
@@ -148,7 +149,7 @@ def _load_model_calls(path: str = MODEL_CALL_PATH):
     try:
         module = _load_module("_model_call", path)
         module.set_entries(*(_address(getattr(_lib, f)) for f in (
-            "ef21_token_logprobs", "ef21_token_logprobs_grad", "ef21_preference_loss_workspace_bytes", "ef21_preference_loss", "ef21_policy_loss_workspace_bytes",
+            "ef21_token_logprobs_workspace_bytes", "ef21_token_logprobs", "ef21_token_logprobs_grad", "ef21_preference_loss_workspace_bytes", "ef21_preference_loss", "ef21_policy_loss_workspace_bytes",
             "ef21_policy_loss", "ef21_balance_loss_workspace_bytes", "ef21_balance_loss", "ef21_embedding", "ef21_embedding_grad_workspace_bytes", "ef21_embedding_grad")))
     except (ImportError, OSError, AttributeError, TypeError) as e:
         warnings.warn(f"losses and embedding without their native calls ({e}): build them with `python -m paper_2106_05203_b200.build`", RuntimeWarning, stacklevel=2)
@@ -626,10 +627,12 @@ def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, scale: float = 1
         with there:
             return token_logprobs(logits, targets, scale, ignore)
     targets, target_stride = _target_rows(targets)
+    nbytes = int(_lib.ef21_token_logprobs_workspace_bytes(dtype, batch, length, vocab))
+    ws, ws_ptr = _workspace(nbytes, device, "ef21_token_logprobs_workspace_bytes")
     logps = torch.empty(targets.shape, dtype=torch.float32, device=device)
     lse = torch.empty(targets.shape, dtype=torch.float32, device=device)
     _check(_lib.ef21_token_logprobs(logits.data_ptr(), dtype, batch, length, vocab, batch_stride, row_stride, targets.data_ptr(), index, target_stride,
-                                    scale, ignore, logps.data_ptr(), lse.data_ptr(), _current_raw_stream(device.index)), "ef21_token_logprobs")
+                                    scale, ignore, logps.data_ptr(), lse.data_ptr(), ws_ptr, nbytes, _current_raw_stream(device.index)), "ef21_token_logprobs")
     return logps, lse
 
 

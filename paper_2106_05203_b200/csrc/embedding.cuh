@@ -252,7 +252,7 @@ struct Columns {
     __device__ __forceinline__ bool in(int k) const { return at(k) < dim; }
 };
 
-// Sums over sorted positions [begin, end), in order; two positions in flight.
+// Sums over sorted positions [begin, end), in order; two (16-bit vectors), four or eight (single elements) positions in flight.
 template <typename T, int VEC>
 __device__ __forceinline__ void add_run(const T* grad, i64 stride, const int2* sorted, int begin, int end, const Columns<VEC>& c, float (&sum)[ED_VECS][VEC]) {
     int i = begin;
@@ -289,7 +289,10 @@ __device__ __forceinline__ void add_run(const T* grad, i64 stride, const int2* s
         }
         i += N;
     };
-    while (i + 2 <= end) add(Count<2>{});
+    constexpr int N = VEC == 1 ? 8 : VEC == 4 ? 4 : 2;
+    while (i + N <= end) add(Count<N>{});
+    if (N > 4 && i + 4 <= end) add(Count<4>{});
+    if (N > 2 && i + 2 <= end) add(Count<2>{});
     if (i < end) add(Count<1>{});
 }
 

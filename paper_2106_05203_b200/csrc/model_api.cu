@@ -64,6 +64,12 @@ unsigned logprob_cluster(i64 rows, i64 vocab) {
     return C;
 }
 
+// Units of one warp per row, 0 where a row has a warp, a block or a cluster: rows that one warp takes, and batches that end with few rows running alone either way.
+i64 logprob_units(int32_t dtype, i64 rows, i64 vocab) {
+    const i64 bytes = bytes_of(dtype), span = (i64)LP_UNIT * 32 * 16 / bytes;
+    return vocab <= LP_WARP_VOCAB || rows < SMS * 2 ? 0 : ceil_div(vocab, span);
+}
+
 // ---- preference loss: which kernel --------------------------------------------------------------------------------------------------------
 
 // Blocks per pair: one where the pairs fill the device, up to eight of at least PF_PART elements each where they do not.  (A cluster's barriers cost: 512 pairs x
@@ -156,13 +162,20 @@ ef21_status enqueue_sort(cudaStream_t st, const void* tokens, int wide, i64 coun
 
 extern "C" {
 
+size_t ef21_token_logprobs_workspace_bytes(int32_t dtype, int64_t batch, int64_t length, int64_t vocab) {
+    if (!valid_logits(dtype, batch, length, vocab, EF21_INDEX_I64, 1.f)) return 0;
+    const i64 units = logprob_units(dtype, batch * length, vocab);
+    return units == 0 ? ALIGN : align_up(sizeof(float2) * (size_t)(batch * length) * (size_t)units);
+}
+
 ef21_status ef21_token_logprobs(const void* logits_dev, int32_t dtype, int64_t batch, int64_t length, int64_t vocab, int64_t batch_stride, int64_t row_stride,
                                 const void* targets_dev, int32_t index_type, int64_t targets_batch_stride, float scale, int64_t ignore,
-                                float* logps_out_dev, float* lse_out_dev, void* cuda_stream) {
+                                float* logps_out_dev, float* lse_out_dev, void* workspace_dev, size_t workspace_bytes, void* cuda_stream) {
     if (!valid_logits(dtype, batch, length, vocab, index_type, scale)) return EF21_ERR_INVALID_ARG;
     const i64 rows = batch * length;
     if (rows == 0) return EF21_OK;
     if (!logits_dev || !targets_dev || !logps_out_dev || !lse_out_dev || !aligned(logits_dev, bytes_of(dtype))) return EF21_ERR_INVALID_ARG;
+    if (!workspace_fits(workspace_dev, workspace_bytes, ef21_token_logprobs_workspace_bytes(dtype, batch, length, vocab))) return EF21_ERR_WORKSPACE;
     const LogprobShape s{length, vocab, batch_stride, row_stride, targets_batch_stride, ignore, index_type, scale};
     return by_dtype(dtype, [&](auto* type) -> ef21_status {
         typedef typename Pointee<decltype(type)>::type T;
@@ -170,6 +183,11 @@ ef21_status ef21_token_logprobs(const void* logits_dev, int32_t dtype, int64_t b
         cudaStream_t st = stream_of(cuda_stream);
         if (vocab <= LP_WARP_VOCAB) {
             CU(launch(logprobs_warp_kernel<T>, (unsigned)ceil_div(rows, LP_THREADS / 32), LP_THREADS, 0, st, 1, logits, targets_dev, logps_out_dev, lse_out_dev, s, rows));
+        } else if (const i64 per_row = logprob_units(dtype, rows, vocab)) {
+            if (ceil_div(rows * per_row, LP_THREADS / 32) > MOST) return EF21_ERR_UNSUPPORTED;        // (beyond any device's memory)
+            float2* part = static_cast<float2*>(workspace_dev);
+            CU(launch(logprobs_unit_kernel<T>, (unsigned)ceil_div(rows * per_row, LP_THREADS / 32), LP_THREADS, 0, st, 1, logits, targets_dev, part, s, rows * per_row, (int)per_row));
+            CU(launch(logprobs_join_kernel<T>, (unsigned)ceil_div(rows, LP_THREADS / 32), LP_THREADS, 0, st, 1, logits, targets_dev, part, logps_out_dev, lse_out_dev, s, rows, (int)per_row));
         } else {
             const unsigned C = logprob_cluster(rows, vocab);
             CU(launch(logprobs_block_kernel<T>, (unsigned)(rows * C), LP_THREADS, 0, st, C, logits, targets_dev, logps_out_dev, lse_out_dev, s, C));
@@ -197,7 +215,7 @@ ef21_status ef21_token_logprobs_grad(const void* logits_dev, int32_t dtype, int6
                       out_row_stride, rows));
             return EF21_OK;
         }
-        const i64 slab = (i64)LP_THREADS * Elem<T>::VEC * LP_UNROLL * 2, slabs = ceil_div(vocab, slab);
+        const i64 slab = (i64)LP_THREADS * Elem<T>::VEC * LG_UNROLL * 2, slabs = ceil_div(vocab, slab);
         if (rows * slabs > MOST) return EF21_ERR_UNSUPPORTED;         // (more than 2^31 slabs of 16 KB or more: no device holds them)
         CU(launch(logprobs_grad_block_kernel<T>, (unsigned)(rows * slabs), LP_THREADS, 0, st, 1, logits, targets_dev, lse_dev, grad_dev, out, s, out_batch_stride, out_row_stride,
                   (unsigned)slabs, slab));

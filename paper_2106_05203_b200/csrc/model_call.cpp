@@ -18,6 +18,7 @@
 namespace {
 
 struct Entries {
+    decltype(&ef21_token_logprobs_workspace_bytes) token_logprobs_bytes;
     decltype(&ef21_token_logprobs) token_logprobs;
     decltype(&ef21_token_logprobs_grad) token_logprobs_grad;
     decltype(&ef21_preference_loss_workspace_bytes) preference_bytes;
@@ -127,13 +128,14 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor &x = THPVariable_Unpack(a[0]), &targets = THPVariable_Unpack(a[1]);
     Rows r;
     if (!r.from(x, targets)) Py_RETURN_NONE;
-    at::Tensor logps, lse;
+    at::Tensor logps, lse, ws;
     int status;
     {
         const Released released;
+        const size_t bytes = entry.token_logprobs_bytes(r.dtype, r.batch, r.length, r.vocab);
         logps = call.make(targets.sizes(), at::kFloat); lse = call.make(targets.sizes(), at::kFloat);
         status = entry.token_logprobs(x.data_ptr(), r.dtype, r.batch, r.length, r.vocab, r.batch_stride, r.row_stride, targets.data_ptr(), r.index, r.target_stride, (float)scale, ignore,
-                                      static_cast<float*>(logps.data_ptr()), static_cast<float*>(lse.data_ptr()), call.stream());
+                                      static_cast<float*>(logps.data_ptr()), static_cast<float*>(lse.data_ptr()), call.workspace(bytes, logps, ws), bytes, call.stream());
     }
     return pack(status, {&logps, &lse});
     END_HANDLE_TH_ERRORS

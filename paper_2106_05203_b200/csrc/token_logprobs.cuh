@@ -21,7 +21,9 @@ struct LogprobShape {
 };
 
 constexpr int LP_THREADS = 256;
+constexpr int LP_UNIT = 16;                  // (units) vectors per lane
 constexpr int LP_UNROLL = 4;                // vectors of 16 bytes per thread in flight
+constexpr int LG_UNROLL = 4;                // (gradient)
 constexpr i64 LP_WARP_VOCAB = 2048;         // rows up to this length belong to one warp
 
 // Maximum and sum of 2^((x - m) c) over what a thread has seen; m = -inf: nothing but -inf so far.
@@ -54,37 +56,58 @@ __device__ __forceinline__ void run_one(const T* x, float c, Running& r) {
     r = merge(r, one, c);
 }
 
-// `count` elements from x on, shared by `threads` threads.
-template <typename T>
-__device__ __forceinline__ Running run_span(const T* x, i64 count, float c, int tid, int threads) {
+// N vectors.
+template <typename T, int N>
+__device__ __forceinline__ void run_vectors(const uint4 (&u)[N], float c, Running& r) {
     constexpr int VEC = Elem<T>::VEC;
-    Running r;
-    const i64 head = min((i64)row_head(x), count), vectors = (count - head) / VEC, tail = count - head - vectors * VEC;
-    if (tid < head) run_one(x + tid, c, r);
-    if (tid < tail) run_one(x + count - tail + tid, c, r);
-    const T* body = x + head;
-    for (i64 v = tid; v < vectors; v += (i64)threads * LP_UNROLL) {
+    float top = Elem<T>::top(u[0]);
+#pragma unroll
+    for (int k = 1; k < N; ++k) top = fmaxf(top, Elem<T>::top(u[k]));
+    const float m = fmaxf(r.m, top), base = m == -INFINITY ? 0.f : m;
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        float f[VEC];
+        Elem<T>::unpack(u[k], f);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sum[e % 2] += exp2_fast((f[e] - base) * c);
+    }
+    r.s = r.s * exp2_fast((r.m - base) * c) + (sum[0] + sum[1]);
+    r.m = m;
+}
+
+// Vectors [tid, count) in steps of `threads`, LP_UNROLL at a time.
+template <typename T>
+__device__ __forceinline__ void run_body(const T* body, int count, float c, int tid, int threads, Running& r) {
+    constexpr int VEC = Elem<T>::VEC;
+    const int step = threads * LP_UNROLL, whole = count / step * step;
+    const T* mine = body + tid * VEC;
+    for (int v = 0; v < whole; v += step) {
+        uint4 u[LP_UNROLL];
+#pragma unroll
+        for (int k = 0; k < LP_UNROLL; ++k) u[k] = load_once(mine + ((i64)v + k * threads) * VEC);
+        run_vectors<T>(u, c, r);
+    }
+    if (whole + tid < count) {
         uint4 u[LP_UNROLL];
 #pragma unroll
         for (int k = 0; k < LP_UNROLL; ++k) {
-            const i64 at = v + (i64)k * threads;
-            u[k] = at < vectors ? load_once(body + at * VEC) : make_uint4(Elem<T>::NEG_INF, Elem<T>::NEG_INF, Elem<T>::NEG_INF, Elem<T>::NEG_INF);
+            u[k] = make_uint4(Elem<T>::NEG_INF, Elem<T>::NEG_INF, Elem<T>::NEG_INF, Elem<T>::NEG_INF);
+            if (whole + tid + k * threads < count) u[k] = load_once(mine + ((i64)whole + k * threads) * VEC);
         }
-        float top = Elem<T>::top(u[0]);
-#pragma unroll
-        for (int k = 1; k < LP_UNROLL; ++k) top = fmaxf(top, Elem<T>::top(u[k]));
-        const float m = fmaxf(r.m, top), base = m == -INFINITY ? 0.f : m;
-        float sum = 0.f;
-#pragma unroll
-        for (int k = 0; k < LP_UNROLL; ++k) {
-            float f[VEC];
-            Elem<T>::unpack(u[k], f);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) sum += exp2_fast((f[e] - base) * c);
-        }
-        r.s = r.s * exp2_fast((r.m - base) * c) + sum;
-        r.m = m;
+        run_vectors<T>(u, c, r);
     }
+}
+
+// `count` elements from x on, shared by `threads` threads.
+template <typename T>
+__device__ __forceinline__ Running run_span(const T* x, int count, float c, int tid, int threads) {
+    constexpr int VEC = Elem<T>::VEC;
+    Running r;
+    const int head = min(row_head(x), count), vectors = (count - head) / VEC, tail = count - head - vectors * VEC;
+    if (tid < head) run_one(x + tid, c, r);
+    if (tid < tail) run_one(x + count - tail + tid, c, r);
+    run_body(x + head, vectors, c, tid, threads, r);
     return r;
 }
 
@@ -111,7 +134,57 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_warp_kernel(const T* logi
     const T* x = logits + b * s.batch_stride + t * s.row_stride;
     const bool inside = target >= 0 && target < s.vocab;
     const float xt = inside ? Elem<T>::get(x[target]) : 0.f, c = s.scale * LOG2E;
-    const Running r = warp_merge(run_span(x, s.vocab, c, lane, 32), c);
+    const Running r = warp_merge(run_span(x, (int)s.vocab, c, lane, 32), c);
+    if (lane == 0) write_logprob(r, xt, inside, s.scale, c, logps + row, lse + row);
+}
+
+// Many long rows: a warp takes LP_UNIT aligned vectors per lane of a row and leaves maximum and sum in part[row][unit]; logprobs_join_kernel has a warp per row, and
+// the elements in front of the first and behind the last vector.  Warps wait for nobody, and the last rows do not run alone.
+template <typename T>
+__global__ void __launch_bounds__(LP_THREADS) logprobs_unit_kernel(const T* logits, const void* targets, float2* part, LogprobShape s, i64 units, int per_row) {
+    pdl_wait(logits, targets, part);
+    pdl_trigger();
+    constexpr int VEC = Elem<T>::VEC, SPAN = LP_UNIT * 32;
+    const int lane = threadIdx.x & 31;
+    const i64 unit = (i64)blockIdx.x * (LP_THREADS / 32) + (threadIdx.x >> 5);
+    if (unit >= units) return;
+    const i64 row = unit / per_row, b = row / s.length, t = row - b * s.length;
+    if (index_at(targets, s.wide, b * s.target_stride + t) == s.ignore) return;
+    const T* x = logits + b * s.batch_stride + t * s.row_stride;
+    const int head = row_head(x), vectors = ((int)s.vocab - head) / VEC, begin = (int)(unit - row * per_row) * SPAN;
+    Running r;
+    if (begin < vectors) run_body(x + head + (i64)begin * VEC, min(SPAN, vectors - begin), s.scale * LOG2E, lane, 32, r);
+    r = warp_merge(r, s.scale * LOG2E);
+    if (lane == 0) part[unit] = make_float2(r.m, r.s);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(LP_THREADS) logprobs_join_kernel(const T* logits, const void* targets, const float2* part, float* logps, float* lse, LogprobShape s, i64 rows, int per_row) {
+    pdl_wait(logits, targets, part, logps, lse);
+    pdl_trigger();
+    const int lane = threadIdx.x & 31;
+    const i64 row = (i64)blockIdx.x * (LP_THREADS / 32) + (threadIdx.x >> 5);
+    if (row >= rows) return;
+    const i64 b = row / s.length, t = row - b * s.length;
+    const i64 target = index_at(targets, s.wide, b * s.target_stride + t);
+    if (target == s.ignore) {
+        if (lane == 0) { logps[row] = 0.f; lse[row] = 0.f; }
+        return;
+    }
+    const bool inside = target >= 0 && target < s.vocab;
+    const T* x = logits + b * s.batch_stride + t * s.row_stride;
+    const float xt = inside ? Elem<T>::get(x[target]) : 0.f, c = s.scale * LOG2E;
+    const int head = row_head(x), behind = head + ((int)s.vocab - head) / Elem<T>::VEC * Elem<T>::VEC;
+    Running r;
+    if (lane < head) run_one(x + lane, c, r);
+    if (behind + lane < (int)s.vocab) run_one(x + behind + lane, c, r);
+    for (int u = lane; u < per_row; u += 32) {
+        const float2 p = part[row * per_row + u];
+        Running one;
+        one.m = p.x; one.s = p.y;
+        r = merge(r, one, c);
+    }
+    r = warp_merge(r, c);
     if (lane == 0) write_logprob(r, xt, inside, s.scale, c, logps + row, lse + row);
 }
 
@@ -135,7 +208,7 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_block_kernel(const T* log
     const float c = s.scale * LOG2E;
     const float xt = inside && tid == 0 && rank == 0 ? Elem<T>::get(x[target]) : 0.f;
     const i64 share = (s.vocab + C - 1) / C, begin = min(rank * share, s.vocab), end = min(begin + share, s.vocab);
-    Running r = warp_merge(run_span(x + begin, end - begin, c, tid, LP_THREADS), c);
+    Running r = warp_merge(run_span(x + begin, (int)(end - begin), c, tid, LP_THREADS), c);
     if ((tid & 31) == 0) part[tid >> 5] = r;
     __syncthreads();
     if (tid < 32) {
@@ -191,15 +264,15 @@ __device__ __forceinline__ void grad_span(const T* x, T* out, i64 begin, i64 end
     if (tid < head) one(begin + tid);
     if (tid < tail) one(end - tail + tid);
     const i64 body = begin + head;
-    for (i64 v = tid; v < vectors; v += (i64)threads * LP_UNROLL) {
-        uint4 u[LP_UNROLL];
+    for (i64 v = tid; v < vectors; v += (i64)threads * LG_UNROLL) {
+        uint4 u[LG_UNROLL];
 #pragma unroll
-        for (int k = 0; k < LP_UNROLL; ++k) {
+        for (int k = 0; k < LG_UNROLL; ++k) {
             const i64 at = v + (i64)k * threads;
             if (at < vectors && !r.zero) u[k] = load_once(x + body + at * VEC);
         }
 #pragma unroll
-        for (int k = 0; k < LP_UNROLL; ++k) {
+        for (int k = 0; k < LG_UNROLL; ++k) {
             const i64 at = v + (i64)k * threads, j = body + at * VEC;
             if (at >= vectors) break;
             if (r.zero) { store_vec(out + j, make_uint4(0u, 0u, 0u, 0u)); continue; }

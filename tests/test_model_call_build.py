@@ -39,7 +39,7 @@ def test_entries_are_looked_at():
     with pytest.raises(TypeError):
         binding._model_calls.set_entries(1, 2)
     with pytest.raises(ValueError):
-        binding._model_calls.set_entries(*[0] * 11)
+        binding._model_calls.set_entries(*[0] * 12)
     assert binding._model_calls.embedding() is None
 
 

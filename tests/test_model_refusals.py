@@ -14,11 +14,15 @@ NAN, INF = float("nan"), float("inf")
 
 
 def test_token_logprobs_entry():
-    good = dict(logits=P, dtype=1, batch=2, length=3, vocab=10, bs=30, rs=10, targets=P, index=1, ts=3, scale=1.0, ignore=-100, logps=P, lse=P, stream=None)
+    good = dict(logits=P, dtype=1, batch=2, length=3, vocab=10, bs=30, rs=10, targets=P, index=1, ts=3, scale=1.0, ignore=-100, logps=P, lse=P, ws=P, n=1 << 20, stream=None)
     for bad in (dict(dtype=3), dict(dtype=-1), dict(batch=-1), dict(length=-1), dict(vocab=0), dict(vocab=1 << 31), dict(batch=1 << 31), dict(batch=1 << 20, length=1 << 20), dict(index=2),
                 dict(scale=0.0), dict(scale=-1.0), dict(scale=NAN), dict(scale=INF), dict(logits=None), dict(logits=P + 1), dict(targets=None), dict(logps=None), dict(lse=None)):
         assert L.ef21_token_logprobs(*{**good, **bad}.values()) == INVALID, bad
     assert L.ef21_token_logprobs(*{**good, "batch": 0, "logits": None}.values()) == 0
+    size = L.ef21_token_logprobs_workspace_bytes
+    assert size(0, 2, 3, 10) > 0 and size(1, 64, 1000, 50000) > 64000 * 8 and size(3, 2, 3, 10) == 0 and size(0, -1, 3, 10) == 0 and size(0, 2, 3, 0) == 0
+    for bad in (dict(ws=None), dict(ws=P + 1), dict(n=8)):
+        assert L.ef21_token_logprobs(*{**good, **bad}.values()) == WORKSPACE, bad
     good = dict(logits=P, dtype=1, batch=2, length=3, vocab=10, bs=30, rs=10, targets=P, index=1, ts=3, lse=P, grad=P, scale=1.0, ignore=-100, out=P, obs=30, ors=10, stream=None)
     for bad in (dict(dtype=3), dict(vocab=0), dict(scale=NAN), dict(lse=None), dict(grad=None), dict(out=None), dict(out=P + 1), dict(index=-1)):
         assert L.ef21_token_logprobs_grad(*{**good, **bad}.values()) == INVALID, bad
