@@ -88,6 +88,7 @@ __global__ void __launch_bounds__(BL_THREADS, PER * VEC <= 16 ? 3 : 1) balance_k
     pdl_trigger();
     __shared__ float column[BL_MAX_EXPERTS];
     __shared__ int here[BL_MAX_EXPERTS];
+    extern __shared__ float of_warp[];                                // [warps][E]
     __shared__ unsigned seen;
     __shared__ double terms, scratch[BL_THREADS / 32];
     const int tid = threadIdx.x, lanes = LANES ? LANES : s.lanes, lane = tid & (lanes - 1), group = tid / lanes, groups = BL_THREADS / lanes, E = s.experts;
@@ -245,18 +246,25 @@ __global__ void __launch_bounds__(BL_THREADS, PER * VEC <= 16 ? 3 : 1) balance_k
 #pragma unroll
         for (int i = 0; i < PAIRS; ++i) sum[i] = add2(sum[i], __shfl_xor_sync(0xffffffffu, sum[i], o));
     }
-    for (int w = 0; w < BL_THREADS / 32; ++w) {
-        if (tid >> 5 == w && (tid & 31) < lanes) {
-            auto add = [&](int e, float v) { if (e < E) column[e] = w == 0 ? v : column[e] + v; };
+    if ((tid & 31) < lanes) {
+        float* mine = of_warp + (tid >> 5) * E;
 #pragma unroll
-            for (int i = 0; i < PAIRS; ++i) {
-                float a, b;
-                split(sum[i], a, b);
-                if (VEC > 1) { add(column_of(2 * i), a); add(column_of(2 * i + 1), b); } else add(column_of(i), a);
-            }
+        for (int i = 0; i < PAIRS; ++i) {
+            float a, b;
+            split(sum[i], a, b);
+            const int e = column_of(VEC > 1 ? 2 * i : i);
+            if (e < E) mine[e] = a;
+            if (VEC > 1 && e + 1 < E) mine[e + 1] = b;
         }
-        __syncthreads();
     }
+    __syncthreads();
+    for (int e = tid; e < E; e += BL_THREADS) {
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < BL_THREADS / 32; ++w) v += of_warp[w * E + e];
+        column[e] = v;
+    }
+    __syncthreads();
     if (!s.one) {
         for (int e = tid; e < E; e += BL_THREADS) partial[(i64)blockIdx.x * E + e] = column[e];
         return;

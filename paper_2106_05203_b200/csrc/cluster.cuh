@@ -34,20 +34,6 @@ __device__ __forceinline__ float remote_float(const float* mine, unsigned rank) 
     asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote_address(mine, rank)) : "memory");
     return v;
 }
-__device__ __forceinline__ int remote_int(const int* mine, unsigned rank) {
-    int v;
-    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(remote_address(mine, rank)) : "memory");
-    return v;
-}
-__device__ __forceinline__ int2 remote_int2(const int2* mine, unsigned rank) {
-    int2 v;
-    asm volatile("ld.shared::cluster.v2.s32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(remote_address(mine, rank)) : "memory");
-    return v;
-}
-__device__ __forceinline__ void remote_store(int2* mine, unsigned rank, int2 v) {
-    asm volatile("st.shared::cluster.v2.s32 [%0], {%1, %2};" ::"r"(remote_address(mine, rank)), "r"(v.x), "r"(v.y) : "memory");
-}
-
 // Sums over the blocks of the cluster, in their order, in thread 0 of rank 0; v counts in thread 0 of every block.  mine: N doubles of shared memory.
 template <int N>
 __device__ __forceinline__ void cluster_sums(double (&v)[N], double* mine) {

@@ -37,21 +37,6 @@ constexpr i64 GRAPH_MAX_D = 512;
 // Workspace layouts
 // ---------------------------------------------------------------------------------------------
 
-// Opt-in of a kernel to more dynamic shared memory than the default 48 KB (and to clusters of more than eight blocks): an
-// attribute per device, set once.
-ef21_status allow_smem(const void* kern, size_t bytes, bool big_cluster = false) {
-    static std::mutex mu;
-    static std::set<std::pair<int, const void*>> done;
-    int dev = -1;
-    CU(cudaGetDevice(&dev));
-    std::lock_guard<std::mutex> lock(mu);
-    if (done.count({dev, kern})) return EF21_OK;
-    CU(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
-    if (big_cluster) CU(cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-    done.insert({dev, kern});
-    return EF21_OK;
-}
-
 struct TopkLayout {
     size_t state, hist, chunks, total;
     int nchunks;

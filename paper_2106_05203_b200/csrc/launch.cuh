@@ -5,6 +5,10 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <mutex>
+#include <set>
+#include <utility>
+
 #include "common.cuh"
 
 #define CU(call)                                         \
@@ -36,6 +40,21 @@ cudaError_t launch(void (*kern)(Params...), dim3 grid, unsigned block, size_t sm
     attr[1].val.clusterDim.x = C; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = C > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kern, static_cast<Params>(args)...);
+}
+
+// Opt-in of a kernel to more dynamic shared memory than the default 48 KB (and to clusters of more than eight blocks): an
+// attribute per device, set once.
+inline ef21_status allow_smem(const void* kern, size_t bytes, bool big_cluster = false) {
+    static std::mutex mu;
+    static std::set<std::pair<int, const void*>> done;
+    int dev = -1;
+    CU(cudaGetDevice(&dev));
+    std::lock_guard<std::mutex> lock(mu);
+    if (done.count({dev, kern})) return EF21_OK;
+    CU(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    if (big_cluster) CU(cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    done.insert({dev, kern});
+    return EF21_OK;
 }
 
 }  // namespace ef21

@@ -141,7 +141,7 @@ bool valid_table(i64 count, i64 vocab, i64 dim) {
 // Sorted positions and the runs of all tokens.
 ef21_status enqueue_sort(cudaStream_t st, const void* tokens, int wide, i64 count, i64 vocab, i64 padding, const EmbeddingWork& w) {
     if (count <= ED_RANK_TOKENS) {
-        CU(launch(embedding_rank_kernel, grid_of(count, ED_RANK_THREADS / 32, SMS * 4), ED_RANK_THREADS, (size_t)count * sizeof(int), st, 1, tokens, wide, (int)count, vocab, padding,
+        CU(launch(embedding_rank_kernel, grid_of(count, ED_RANK_THREADS / 32, SMS * 4), ED_RANK_THREADS, (size_t)ceil_div(count, 128) * 128 * sizeof(int), st, 1, tokens, wide, (int)count, vocab, padding,
                   w.sorted, w.runs));
         return EF21_OK;
     }
@@ -342,7 +342,7 @@ ef21_status ef21_balance_loss(const void* logits_dev, int32_t dtype, int64_t row
             CU(launch(balance_count_kernel, grid_of(rows * chosen, BL_COUNT_THREADS * 4, SMS * 2), BL_COUNT_THREADS, 0, st, 1, choices_dev, mask_dev, counts_out_dev, w.work, s));
         }
         auto run = [&](auto kernel) -> ef21_status {
-            CU(launch(kernel, blocks, BL_THREADS, 0, st, s.one ? blocks : 1, logits, choices_dev, mask_dev, counts_out_dev, w.work, grad, w.partial, probs_out_dev, loss_out_dev, s));
+            CU(launch(kernel, blocks, BL_THREADS, sizeof(float) * (size_t)(BL_THREADS / 32 * experts), st, s.one ? blocks : 1, logits, choices_dev, mask_dev, counts_out_dev, w.work, grad, w.partial, probs_out_dev, loss_out_dev, s));
             return EF21_OK;
         };
         // rows in flight per team: 16 values per lane or more

@@ -63,12 +63,12 @@ __global__ void __launch_bounds__(PO_COUNT_THREADS) policy_count_kernel(const un
         const i64 vectors = (length - head) / 16, tail = head + vectors * 16;
         int n = 0;
         if (lane < head) n += m[lane] != 0;
-        for (i64 v = lane; v < vectors; v += 4 * 32) {
-            uint4 u[4];
+        for (i64 v = lane; v < vectors; v += 8 * 32) {
+            uint4 u[8];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) u[k] = v + k * 32 < vectors ? *reinterpret_cast<const uint4*>(m + head + (v + k * 32) * 16) : make_uint4(0u, 0u, 0u, 0u);
+            for (int k = 0; k < 8; ++k) u[k] = v + k * 32 < vectors ? *reinterpret_cast<const uint4*>(m + head + (v + k * 32) * 16) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) n += count_bytes(u[k].x) + count_bytes(u[k].y) + count_bytes(u[k].z) + count_bytes(u[k].w);
+            for (int k = 0; k < 8; ++k) n += count_bytes(u[k].x) + count_bytes(u[k].y) + count_bytes(u[k].z) + count_bytes(u[k].w);
         }
         if (tail + lane < length) n += m[tail + lane] != 0;
         n = __reduce_add_sync(0xffffffffu, n);
