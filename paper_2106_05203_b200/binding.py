@@ -578,6 +578,23 @@ def _elsewhere(device: torch.device, stream: Optional[torch.cuda.Stream]):
     return None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
 
+def _rows_apart(t: torch.Tensor, name: str) -> None:
+    """Refuses a tensor some of whose rows lie on one another: every stride must step over all that the smaller ones reach."""
+    reach = t.shape[-1]
+    for size, stride in sorted(((n, s) for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n > 1), key=lambda p: p[1]):
+        if stride < reach:
+            raise ValueError(f"rows of {name} overlap")
+        reach += (size - 1) * stride
+
+
+def _overlap(a: torch.Tensor, b: torch.Tensor) -> bool:
+    """Whether the stretches of memory from the first to the last element of two tensors meet."""
+    if a.numel() == 0 or b.numel() == 0:
+        return False
+    (x, y), (u, v) = ((t.data_ptr(), t.data_ptr() + (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))) * t.element_size()) for t in (a, b))
+    return x < v and u < y
+
+
 def _workspace(nbytes: int, device: torch.device, where: str):
     """A workspace, and its 256-byte aligned address."""
     if nbytes == 0:
@@ -655,8 +672,9 @@ def token_logprobs_grad(logits: torch.Tensor, targets: torch.Tensor, lse: torch.
     if out is not None:
         if out.shape != logits.shape or out.dtype != logits.dtype:
             raise ValueError("out must have the logits' shape and type")
-        if any(n > 1 and st < vocab for n, st in zip(out.shape[:-1], out.stride()[:-1])):
-            raise ValueError("rows of out overlap")
+        _rows_apart(out, "out")
+        if not (out.data_ptr() == logits.data_ptr() and out.stride() == logits.stride()) and _overlap(out, logits):
+            raise ValueError("out must be the logits, or apart from them")
     device = _same_device(logits, targets, lse, grad, out)
     there = _elsewhere(device, stream)
     if there is not None:
@@ -842,8 +860,9 @@ def embedding_grad(grad: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: 
         raise TypeError(f"the result must be of grad's type or float32, not {result}")
     if out is not None:
         out_stride = _matrix(out, "out", (vocab, dim))
-        if vocab > 1 and out_stride < dim:
-            raise ValueError("rows of out overlap")
+        _rows_apart(out, "out")
+        if _overlap(out, grad):
+            raise ValueError("out must be apart from grad")
     device = _same_device(grad, tokens, out)
     there = _elsewhere(device, stream)
     if there is not None:

@@ -21,7 +21,7 @@ constexpr int ED_SUM_THREADS = 64;          // (a block keeps its place until it
 constexpr int ED_CHUNK = 32;                // sorted positions that one team adds up
 constexpr int ED_VECS = 2;                  // vectors per lane and row
 constexpr int ED_ROW_VECS = 4;
-constexpr int ED_SHARES = ED_THREADS / 32;
+constexpr int ED_JOIN_THREADS = 512, ED_SHARES = ED_JOIN_THREADS / 32;
 constexpr int ED_ROWS = 4;                  // rows of the table per team
 constexpr int ED_RANK_TOKENS = 4096;
 constexpr int ED_RANK_THREADS = 256;
@@ -270,18 +270,18 @@ template <typename O, int VEC> __device__ __forceinline__ void put_elements(O* o
     }
 }
 
-// The columns of one lane: ED_VECS vectors, a team's lanes side by side.
-template <int VEC>
+// The columns of one lane: VECS vectors, a team's lanes side by side.
+template <int VEC, int VECS>
 struct Columns {
     i64 first, step, dim;
-    __device__ __forceinline__ Columns(const TableShape& s, int slab, int lane) : first(((i64)slab * ED_VECS * s.lanes + lane) * VEC), step((i64)s.lanes * VEC), dim(s.dim) {}
+    __device__ __forceinline__ Columns(const TableShape& s, int slab, int lane) : first(((i64)slab * VECS * s.lanes + lane) * VEC), step((i64)s.lanes * VEC), dim(s.dim) {}
     __device__ __forceinline__ i64 at(int k) const { return first + k * step; }
     __device__ __forceinline__ bool in(int k) const { return at(k) < dim; }
 };
 
 // Sums over sorted positions [begin, end), in order; two (16-bit vectors), four or eight (single elements) positions in flight.
 template <typename T, int VEC>
-__device__ __forceinline__ void add_run(const T* grad, i64 stride, const int2* sorted, int begin, int end, const Columns<VEC>& c, float (&sum)[ED_VECS][VEC]) {
+__device__ __forceinline__ void add_run(const T* grad, i64 stride, const int2* sorted, int begin, int end, const Columns<VEC, ED_VECS>& c, float (&sum)[ED_VECS][VEC]) {
     int i = begin;
     auto add = [&](auto n) {
         constexpr int N = decltype(n)::value;
@@ -328,7 +328,7 @@ template <typename T, int VEC>
 struct First {
     typedef typename std::conditional<(VEC > 1), uint4, float>::type Raw;
     Raw raw[ED_VECS];
-    __device__ __forceinline__ void fetch(const T* g, const Columns<VEC>& c, bool there) {
+    __device__ __forceinline__ void fetch(const T* g, const Columns<VEC, ED_VECS>& c, bool there) {
 #pragma unroll
         for (int k = 0; k < ED_VECS; ++k) {
             if constexpr (VEC > 1) raw[k] = there && c.in(k) ? load_once(g + c.at(k)) : make_uint4(0u, 0u, 0u, 0u);
@@ -345,10 +345,10 @@ struct First {
 };
 
 // One row's columns of a lane: scaled, added to what is there where that is asked for, rounded.
-template <typename O, int VEC>
-__device__ __forceinline__ void put_row(O* row, const Columns<VEC>& c, const float (&sum)[ED_VECS][VEC], const TableShape& s) {
+template <typename O, int VEC, int VECS>
+__device__ __forceinline__ void put_row(O* row, const Columns<VEC, VECS>& c, const float (&sum)[VECS][VEC], const TableShape& s) {
 #pragma unroll
-    for (int k = 0; k < ED_VECS; ++k) {
+    for (int k = 0; k < VECS; ++k) {
         if (!c.in(k)) continue;
         O* o = row + c.at(k);
         float f[VEC];
@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(ED_SUM_THREADS, 12) embedding_sums_kernel(cons
     const bool chunks = before != (unsigned)((unsigned long long)(blockIdx.x + 1) * s.long_blocks / gridDim.x);
     const i64 item = (i64)(chunks ? before : blockIdx.x - before) * teams + team;
     const i64 at = s.slabs == 1 ? item : item / s.slabs;
-    const Columns<VEC> c(s, (int)(item - at * s.slabs), lane);
+    const Columns<VEC, ED_VECS> c(s, (int)(item - at * s.slabs), lane);
     if (chunks) {
         const i64 c0 = at * ED_CHUNK, c1 = min(c0 + ED_CHUNK, s.count);
         if (c0 >= s.count) return;
@@ -423,33 +423,35 @@ __global__ void __launch_bounds__(ED_SUM_THREADS, 12) embedding_sums_kernel(cons
     }
 }
 
-// A run's first chunk holds it last (`second`), unless the run begins where the chunk does; every other one first.
+// Adds up the partial sums of chunks [begin, end), four on their way at a time.  A run's first chunk holds it last (`first` is that chunk, where the run does not begin
+// with it; else -1), every other one first.
 template <int VEC>
-__device__ __forceinline__ void add_partial(const float* partial, i64 chunk, bool second, const Columns<VEC>& c, float (&sum)[ED_VECS][VEC]) {
-    const float* p = partial + (chunk * 2 + second) * c.dim;
+__device__ __forceinline__ void add_partials(const float* partial, int begin, int end, int first, const Columns<VEC, 1>& c, float (&sum)[1][VEC]) {
+    if (!c.in(0)) return;
+    for (int i = begin; i < end; i += 4) {
+        float f[4][VEC] = {};
 #pragma unroll
-    for (int k = 0; k < ED_VECS; ++k) {
-        if (!c.in(k)) continue;
-        float f[VEC];
-        get_floats<VEC>(p + c.at(k), f);
+        for (int k = 0; k < 4; ++k) if (i + k < end) get_floats<VEC>(partial + ((i64)(i + k) * 2 + (i + k == first)) * c.dim + c.at(0), f[k]);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sum[k][e] += f[e];
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum[0][e] += f[k][e];
     }
 }
 
 // The long runs, by their first chunk (a long run that begins in a chunk is its last one): a block looks through ED_SHARES chunks at once and joins, slab by slab
 // of blockIdx.y, what begins there.  ED_SHARES teams (a block has that many or more) add up a share of the run's chunks each, in order, then the
-// shares are added in order: the same order however wide a team is.
+// shares are added in order: the same order however wide a team is.  One vector a lane: the partial sums of a run come from memory, the more of them at once the better.
 template <typename O, int VEC>
-__global__ void __launch_bounds__(ED_THREADS) embedding_join_kernel(const int2* sorted, const int2* runs, const float* partial, O* out, TableShape s) {
+__global__ void __launch_bounds__(ED_JOIN_THREADS) embedding_join_kernel(const int2* sorted, const int2* runs, const float* partial, O* out, TableShape s) {
     pdl_wait(sorted, runs, partial, out);
     pdl_trigger();
-    __shared__ float shares[ED_THREADS * ED_VECS * VEC];           // (ED_SHARES teams of up to 32 lanes)
+    __shared__ float shares[ED_JOIN_THREADS * VEC];                // (ED_SHARES teams of up to 32 lanes)
     __shared__ int2 found[ED_SHARES];
     __shared__ int keys[ED_SHARES];
+    int2 run = make_int2(0, 0);
     if (threadIdx.x < ED_SHARES) {
         const i64 c0 = ((i64)blockIdx.x * ED_SHARES + threadIdx.x) * ED_CHUNK;
-        int2 run = make_int2(0, 0);
         int key = 0;
         if (c0 < s.count) {
             key = sorted[min(c0 + ED_CHUNK, s.count) - 1].x;
@@ -459,42 +461,39 @@ __global__ void __launch_bounds__(ED_THREADS) embedding_join_kernel(const int2* 
         found[threadIdx.x] = run;
         keys[threadIdx.x] = key;
     }
-    __syncthreads();
+    const int chunks_of = run.y == 0 ? 0 : (run.y - 1) / ED_CHUNK - run.x / ED_CHUNK + 1;
+    if (!__syncthreads_or(chunks_of)) return;
+    const bool longest = __syncthreads_or(chunks_of > ED_SHARES);
     const int lane = threadIdx.x & (s.lanes - 1), team = threadIdx.x / s.lanes;
-    const Columns<VEC> c(s, blockIdx.y, lane);
+    const Columns<VEC, 1> c(s, blockIdx.y, lane);
     // runs of up to ED_SHARES chunks: a team each, a share being a chunk
     if (team < ED_SHARES && found[team].y != 0) {
         const int2 run = found[team];
         const int chunk = run.x / ED_CHUNK, n = (run.y - 1) / ED_CHUNK - chunk + 1;
         if (n <= ED_SHARES) {
-            float sum[ED_VECS][VEC] = {};
-#pragma unroll 4
-            for (int i = chunk; i < chunk + n; ++i) add_partial(partial, i, i == chunk && run.x > chunk * ED_CHUNK, c, sum);
+            float sum[1][VEC] = {};
+            add_partials(partial, chunk, chunk + n, run.x > chunk * ED_CHUNK ? chunk : -1, c, sum);
             put_row<O, VEC>(out + (i64)keys[team] * s.out_stride, c, sum, s);
         }
     }
+    if (!longest) return;
     for (int w = 0; w < ED_SHARES; ++w) {
         const int2 run = found[w];
         const int chunk = run.x / ED_CHUNK, n = (run.y - 1) / ED_CHUNK - chunk + 1, per = (n + ED_SHARES - 1) / ED_SHARES;
         if (run.y == 0 || n <= ED_SHARES) continue;                // (the same in all threads)
         const int begin = chunk + min(team * per, n), end = chunk + min((team + 1) * per, n);
-        float* mine = shares + (size_t)team * s.lanes * ED_VECS * VEC + lane;                      // [team][vector][element][lane]
-        float sum[ED_VECS][VEC] = {};
+        float* mine = shares + (size_t)team * s.lanes * VEC + lane;                                // [team][element][lane]
+        float sum[1][VEC] = {};
         if (team < ED_SHARES) {
-#pragma unroll 4
-            for (int i = begin; i < end; ++i) add_partial(partial, i, i == chunk && run.x > chunk * ED_CHUNK, c, sum);
+            add_partials(partial, begin, end, run.x > chunk * ED_CHUNK ? chunk : -1, c, sum);
 #pragma unroll
-            for (int k = 0; k < ED_VECS; ++k)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) mine[(k * VEC + e) * s.lanes] = sum[k][e];
+            for (int e = 0; e < VEC; ++e) mine[e * s.lanes] = sum[0][e];
         }
         __syncthreads();
         if (team == 0) {
             for (int t = 1; t < min(ED_SHARES, n); ++t)
 #pragma unroll
-                for (int k = 0; k < ED_VECS; ++k)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) sum[k][e] += mine[(size_t)t * s.lanes * ED_VECS * VEC + (k * VEC + e) * s.lanes];
+                for (int e = 0; e < VEC; ++e) sum[0][e] += mine[(size_t)t * s.lanes * VEC + e * s.lanes];
             put_row<O, VEC>(out + (i64)keys[w] * s.out_stride, c, sum, s);
         }
         __syncthreads();

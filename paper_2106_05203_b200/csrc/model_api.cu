@@ -413,14 +413,18 @@ ef21_status ef21_embedding_grad(const void* grad_dev, int32_t dtype, int64_t cou
             s.slabs = (int)ceil_div(columns, (i64)s.lanes * ED_VECS);
             const i64 teams = ED_SUM_THREADS / s.lanes, chunks = count > ED_CHUNK ? ceil_div(count, ED_CHUNK) : 0;
             const i64 long_blocks = ceil_div(chunks * s.slabs, teams), row_blocks = ceil_div(ceil_div(vocab, ED_ROWS) * s.slabs, teams);
-            if (long_blocks + row_blocks > MOST || s.slabs > 65535) return EF21_ERR_UNSUPPORTED;      // (beyond any device's memory)
+            if (long_blocks + row_blocks > MOST || columns > 65535ll * 32) return EF21_ERR_UNSUPPORTED;      // (beyond any device's memory; rows of two million columns)
             s.long_blocks = (unsigned)long_blocks;
             const unsigned blocks = (unsigned)(long_blocks + row_blocks);
             if (vectors) CU(launch(embedding_sums_kernel<T, O, true>, blocks, ED_SUM_THREADS, 0, st, 1, grad, w.sorted, w.runs, w.partial, out, s));
             else CU(launch(embedding_sums_kernel<T, O, false>, blocks, ED_SUM_THREADS, 0, st, 1, grad, w.sorted, w.runs, w.partial, out, s));
             if (chunks == 0) return EF21_OK;
-            if (vectors) CU(launch(embedding_join_kernel<O, VEC>, dim3((unsigned)ceil_div(chunks, ED_SHARES), s.slabs), ED_THREADS, 0, st, 1, w.sorted, w.runs, w.partial, out, s));
-            else CU(launch(embedding_join_kernel<O, 1>, dim3((unsigned)ceil_div(chunks, ED_SHARES), s.slabs), ED_THREADS, 0, st, 1, w.sorted, w.runs, w.partial, out, s));
+            s.lanes = 1;                                              // the join's teams: one vector a lane
+            while (s.lanes < 32 && s.lanes < columns) s.lanes *= 2;
+            s.slabs = (int)ceil_div(columns, s.lanes);
+            const dim3 grid((unsigned)ceil_div(chunks, ED_SHARES), (unsigned)s.slabs);
+            if (vectors) CU(launch(embedding_join_kernel<O, VEC>, grid, ED_JOIN_THREADS, 0, st, 1, w.sorted, w.runs, w.partial, out, s));
+            else CU(launch(embedding_join_kernel<O, 1>, grid, ED_JOIN_THREADS, 0, st, 1, w.sorted, w.runs, w.partial, out, s));
             return EF21_OK;
         };
         return out_dtype == EF21_DTYPE_F32 ? run(static_cast<float*>(out_dev)) : run(static_cast<T*>(out_dev));

@@ -42,7 +42,7 @@ def test_against_the_definition(B, dtype, rows, vocab):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("batch,length,vocab", [(3, 5, 4097), (2, 1, 33), (4, 9, 2500), (1, 12, 50257)])
+@pytest.mark.parametrize("batch,length,vocab", [(3, 5, 4097), (2, 1, 33), (4, 9, 2500), (1, 12, 50257), (40, 9, 4099), (3, 100, 9001)])
 def test_views_of_a_batch(B, dtype, batch, length, vocab):
     """Every position against the token behind it: no row of the last position is touched; gradients into a view of a table of their own."""
     g = generator(vocab)

@@ -99,6 +99,9 @@ def i(*shape, dtype=torch.int64):
     (ValueError, lambda: B.token_logprobs_grad(f(2, 3), i(2), f(3), f(2))),
     (ValueError, lambda: B.token_logprobs_grad(f(2, 3), i(2), f(2), f(2), out=f(3, 3))),
     (ValueError, lambda: B.token_logprobs_grad(f(2, 3), i(2), f(2), f(2), out=f(1, 3).expand(2, 3))),
+    (ValueError, lambda: (lambda x: B.token_logprobs_grad(x[:, :-1], i(4, 5), f(4, 5), f(4, 5), out=x[:, 1:]))(f(4, 6, 8))),
+    (ValueError, lambda: (lambda x: B.token_logprobs_grad(x[:4], i(4), f(4), f(4), out=x[1:]))(f(5, 8))),
+    (ValueError, lambda: B.token_logprobs_grad(f(2, 2, 8), i(2, 2), f(2, 2), f(2, 2), out=f(100).as_strided((2, 2, 8), (8, 8, 1)))),
     (ValueError, lambda: B.preference_loss(f(3, 4))),
     (ValueError, lambda: B.preference_loss(f(0, 4))),
     (ValueError, lambda: B.preference_loss(f(4))),
@@ -128,6 +131,7 @@ def i(*shape, dtype=torch.int64):
     (ValueError, lambda: B.embedding_grad(f(4, 3), i(4), 10, out=f(9, 3))),
     (ValueError, lambda: B.embedding_grad(f(4, 3), i(4), 10, out=f(1, 3).expand(10, 3))),
     (ValueError, lambda: B.embedding_grad(f(4, 3), i(4), 10, accumulate=True)),
+    (ValueError, lambda: (lambda x: B.embedding_grad(x[:4], i(4), 4, out=x[2:6]))(f(6, 3))),
     (TypeError, lambda: B.embedding_grad(f(2, 3, 8)[:, :2], i(2, 2), 10)),
 ], ids=lambda v: "" if not isinstance(v, type) else v.__name__)
 def test_the_binding_refuses(error, call):
