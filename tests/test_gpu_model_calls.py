@@ -72,7 +72,7 @@ def test_the_current_stream_is_taken(B):
 def test_parameters_and_gradients(B):
     """A subclass takes the general call; results are constants of autograd either way."""
     for name, (call, args) in calls(B).items():
-        want = flat(call(*args))
+        want = flat(call(args[0].detach().clone(), *args[1:]))         # (in the clones' layout: a row's sums are in an order that goes by its alignment)
         leaf = args[0].detach().clone().requires_grad_()
         for first in (torch.nn.Parameter(args[0].detach().clone()), leaf):
             got = flat(call(first, *args[1:]))

@@ -93,6 +93,18 @@ def test_masked_and_non_finite_logits(B, dtype, vocab):
     assert not bool(B.token_logprobs_grad(logits, targets, lse, torch.zeros(10, device="cuda")).any())      # NaN in rows without a gradient
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab", [(3, 77), (2, 30000), (300, 4100)])
+def test_a_target_that_a_mask_took(B, dtype, rows, vocab):
+    """Of the type's lowest value: its log-probability is that value (times the scale), less the row's lse -- a finite number."""
+    logits = torch.randn(rows, vocab, device="cuda", generator=generator(vocab)).to(dtype)
+    logits[:, ::2] = torch.finfo(dtype).min
+    targets = torch.arange(rows, device="cuda") % (vocab // 2) * 2
+    for scale in (1.0, 0.5):
+        logp, lse, grad, dx = check(B, logits, targets, scale=scale)
+        assert bool(torch.isfinite(logp).all()) and bool((logp < scale * 0.99 * torch.finfo(dtype).min).all())
+
+
 def test_large_logits_and_int32(B):
     logits = torch.full((3, 3000), 30000.0, device="cuda"); logits[1] = -30000.0; logits[2, 1700] = 30100.0
     targets = torch.tensor([5, 2999, 1700], device="cuda", dtype=torch.int32)
