@@ -261,8 +261,6 @@ template <int VEC> __device__ __forceinline__ void get_floats(const float* p, fl
     }
 }
 
-template <int N> struct Count { static constexpr int value = N; };
-
 // VEC elements of a row of the table: 16 bytes, or 32 (fp32 from 16-bit gradients), or one element.
 template <typename O, int VEC> __device__ __forceinline__ void put_elements(O* o, const float (&f)[VEC]) {
     if constexpr (sizeof(O) == 4) put_floats<VEC>(o, f);
@@ -282,21 +280,25 @@ struct Columns {
     __device__ __forceinline__ bool in(int k) const { return at(k) < dim; }
 };
 
-// Sums over sorted positions [begin, end), in order; two (16-bit vectors), four or eight (single elements) positions in flight.
+// Sums over sorted positions [begin, end), in order: two (16-bit vectors), four or eight (single elements) at a time, the next ones' places looked up meanwhile.
 template <typename T, int VEC>
 __device__ __forceinline__ void add_run(const T* grad, i64 stride, const int2* sorted, int begin, int end, const Columns<VEC, ED_VECS>& c, float (&sum)[ED_VECS][VEC]) {
-    int i = begin;
-    auto add = [&](auto n) {
-        constexpr int N = decltype(n)::value;
-        const T* g[N];
+    constexpr int N = VEC == 1 ? 8 : VEC == 4 ? 4 : 2;
+    int at[N];
 #pragma unroll
-        for (int p = 0; p < N; ++p) g[p] = grad + (i64)sorted[i + p].y * stride;
-        if (VEC > 1) {
+    for (int p = 0; p < N; ++p) at[p] = begin + p < end ? sorted[begin + p].y : 0;
+    for (int i = begin; i < end; i += N) {
+        if constexpr (VEC > 1) {
             uint4 u[N][ED_VECS];
 #pragma unroll
             for (int p = 0; p < N; ++p)
 #pragma unroll
-                for (int k = 0; k < ED_VECS; ++k) if (c.in(k)) u[p][k] = load_once(g[p] + c.at(k));
+                for (int k = 0; k < ED_VECS; ++k) {
+                    u[p][k] = make_uint4(0u, 0u, 0u, 0u);
+                    if (i + p < end && c.in(k)) u[p][k] = load_once(grad + (i64)at[p] * stride + c.at(k));
+                }
+#pragma unroll
+            for (int p = 0; p < N; ++p) at[p] = i + N + p < end ? sorted[i + N + p].y : 0;
 #pragma unroll
             for (int p = 0; p < N; ++p)
 #pragma unroll
@@ -311,19 +313,15 @@ __device__ __forceinline__ void add_run(const T* grad, i64 stride, const int2* s
 #pragma unroll
             for (int p = 0; p < N; ++p)
 #pragma unroll
-                for (int k = 0; k < ED_VECS; ++k) f[p][k] = c.in(k) ? Elem<T>::get(g[p][c.at(k)]) : 0.f;
+                for (int k = 0; k < ED_VECS; ++k) f[p][k] = i + p < end && c.in(k) ? Elem<T>::get(grad[(i64)at[p] * stride + c.at(k)]) : 0.f;
+#pragma unroll
+            for (int p = 0; p < N; ++p) at[p] = i + N + p < end ? sorted[i + N + p].y : 0;
 #pragma unroll
             for (int p = 0; p < N; ++p)
 #pragma unroll
                 for (int k = 0; k < ED_VECS; ++k) sum[k][0] += f[p][k];
         }
-        i += N;
-    };
-    constexpr int N = VEC == 1 ? 8 : VEC == 4 ? 4 : 2;
-    while (i + N <= end) add(Count<N>{});
-    if (N > 4 && i + 4 <= end) add(Count<4>{});
-    if (N > 2 && i + 2 <= end) add(Count<2>{});
-    if (i < end) add(Count<1>{});
+    }
 }
 
 // A row's first gradient on its way; zeros where there is none.
