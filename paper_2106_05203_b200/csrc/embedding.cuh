@@ -25,7 +25,7 @@ constexpr int ED_CHUNK = 32;                // sorted positions that one team ad
 constexpr int ED_VECS = 2;                  // vectors per lane and row
 constexpr int ED_ROW_VECS = 4;
 constexpr int ED_JOIN_THREADS = 512, ED_SHARES = ED_JOIN_THREADS / 32;
-constexpr int ED_ROWS = 4;                  // rows of the table per team
+constexpr int ED_ROWS = 4;                  // rows of the table per team where that leaves enough teams
 constexpr int ED_RANK_TOKENS = 4096;
 constexpr int ED_RANK_THREADS = 256;
 constexpr int RX_THREADS = 1024, RX_ITEMS = 1, RX_TILE = RX_THREADS * RX_ITEMS, RX_MAX_BITS = 9, RX_WARPS = RX_THREADS / 32;
@@ -280,10 +280,37 @@ struct Columns {
     __device__ __forceinline__ bool in(int k) const { return at(k) < dim; }
 };
 
-// Sums over sorted positions [begin, end), in order: two (16-bit vectors), four or eight (single elements) at a time, the next ones' places looked up meanwhile.
+// Sums over sorted positions [begin, end), in order.  16-bit vectors: two at a time, what is left over alone (registers; whatever else was tried costs the large table 3 %).
+// Others: four or eight (single elements) at a time, the next ones' places looked up meanwhile -- small tables wait for the longest run.
 template <typename T, int VEC>
 __device__ __forceinline__ void add_run(const T* grad, i64 stride, const int2* sorted, int begin, int end, const Columns<VEC, ED_VECS>& c, float (&sum)[ED_VECS][VEC]) {
-    constexpr int N = VEC == 1 ? 8 : VEC == 4 ? 4 : 2;
+    if constexpr (VEC == 8) {
+        auto two_or_one = [&](int i, auto n) {
+            constexpr int N = decltype(n)::value;
+            const T* g[N];
+#pragma unroll
+            for (int p = 0; p < N; ++p) g[p] = grad + (i64)sorted[i + p].y * stride;
+            uint4 u[N][ED_VECS];
+#pragma unroll
+            for (int p = 0; p < N; ++p)
+#pragma unroll
+                for (int k = 0; k < ED_VECS; ++k) if (c.in(k)) u[p][k] = load_once(g[p] + c.at(k));
+#pragma unroll
+            for (int p = 0; p < N; ++p)
+#pragma unroll
+                for (int k = 0; k < ED_VECS; ++k) {
+                    float f[Elem<T>::VEC];
+                    Elem<T>::unpack(u[p][k], f);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) sum[k][e] += f[e];
+                }
+        };
+        int i = begin;
+        for (; i + 2 <= end; i += 2) two_or_one(i, std::integral_constant<int, 2>{});
+        if (i < end) two_or_one(i, std::integral_constant<int, 1>{});
+        return;
+    }
+    constexpr int N = VEC == 1 ? 8 : 4;
     int at[N];
 #pragma unroll
     for (int p = 0; p < N; ++p) at[p] = begin + p < end ? sorted[begin + p].y : 0;
@@ -366,7 +393,7 @@ __device__ __forceinline__ void put_row(O* row, const Columns<VEC, VECS>& c, con
 // long_blocks of the blocks: chunks of ED_CHUNK sorted positions, the sums of the long runs that they cut.  A run longer than a chunk holds the chunk's first
 // or its last position wherever it meets one: partial[chunk][0] belongs to the first position's run, [1] to the last one's where that is another.
 // The others: rows of the table with no or few positions.
-template <typename T, typename O, bool VECTORS>
+template <typename T, typename O, bool VECTORS, int ROWS>
 __global__ void __launch_bounds__(ED_SUM_THREADS, 12) embedding_sums_kernel(const T* grad, const int2* sorted, const int2* runs, float* partial, O* out, TableShape s) {
     pdl_wait(grad, sorted, runs, partial, out);
     pdl_trigger();
@@ -396,27 +423,27 @@ __global__ void __launch_bounds__(ED_SUM_THREADS, 12) embedding_sums_kernel(cons
         }
         return;
     }
-    // ED_ROWS rows, one after the other: their runs are looked up together, and a row's first gradient is on its way while the row before it is formed
-    const i64 first = at * ED_ROWS;
+    // ROWS rows, one after the other: their runs are looked up together, and a row's first gradient is on its way while the row before it is formed
+    const i64 first = at * ROWS;
     if (first >= s.vocab) return;
-    int2 run[ED_ROWS], head[ED_ROWS];
+    int2 run[ROWS], head[ROWS];
 #pragma unroll
-    for (int r = 0; r < ED_ROWS; ++r) {
+    for (int r = 0; r < ROWS; ++r) {
         run[r] = first + r < s.vocab ? runs[first + r] : make_int2(-1, -1);
         head[r] = run[r].x >= 0 && run[r].x < s.count ? sorted[run[r].x] : make_int2(-1, 0);
     }
 #pragma unroll
-    for (int r = 0; r < ED_ROWS; ++r) if (head[r].x != first + r) run[r] = make_int2(0, 0);          // no such token
+    for (int r = 0; r < ROWS; ++r) if (head[r].x != first + r) run[r] = make_int2(0, 0);          // no such token
     First<T, VEC> next;
     next.fetch(grad + (i64)head[0].y * s.stride, c, run[0].y > run[0].x && run[0].y - run[0].x <= ED_CHUNK);
 #pragma unroll
-    for (int r = 0; r < ED_ROWS; ++r) {
+    for (int r = 0; r < ROWS; ++r) {
         const int n = run[r].y - run[r].x;
         float sum[ED_VECS][VEC];
         next.take(sum);
-        if (r + 1 < ED_ROWS) {
-            const int m = run[(r + 1) % ED_ROWS].y - run[(r + 1) % ED_ROWS].x;
-            next.fetch(grad + (i64)head[(r + 1) % ED_ROWS].y * s.stride, c, m > 0 && m <= ED_CHUNK);
+        if (r + 1 < ROWS) {
+            const int m = run[(r + 1) % ROWS].y - run[(r + 1) % ROWS].x;
+            next.fetch(grad + (i64)head[(r + 1) % ROWS].y * s.stride, c, m > 0 && m <= ED_CHUNK);
         }
         if (first + r >= s.vocab || n > ED_CHUNK || (n == 0 && s.accumulate)) continue;
         if (n > 1) add_run<T, VEC>(grad, s.stride, sorted, run[r].x + 1, run[r].y, c, sum);

@@ -412,12 +412,20 @@ ef21_status ef21_embedding_grad(const void* grad_dev, int32_t dtype, int64_t cou
             while (s.lanes < 32 && (i64)s.lanes * ED_VECS < columns) s.lanes *= 2;
             s.slabs = (int)ceil_div(columns, (i64)s.lanes * ED_VECS);
             const i64 teams = ED_SUM_THREADS / s.lanes, chunks = count > ED_CHUNK ? ceil_div(count, ED_CHUNK) : 0;
-            const i64 long_blocks = ceil_div(chunks * s.slabs, teams), row_blocks = ceil_div(ceil_div(vocab, ED_ROWS) * s.slabs, teams);
+            const i64 long_blocks = ceil_div(chunks * s.slabs, teams), warps = ceil_div(vocab * s.slabs * s.lanes, 32);
+            // a row after the other is worth it where the device has its fill of warps all the same (50,000 tokens' rows of 8 columns, which fill a quarter of it: 24 us for 4,000
+            // positions four rows at a time, as long as the longest runs of four rows take)
+            const int per_team = warps >= (i64)SMS * 24 * ED_ROWS ? ED_ROWS : 1;
+            const i64 row_blocks = ceil_div(ceil_div(vocab, per_team) * s.slabs, teams);
             if (long_blocks + row_blocks > MOST || columns > 65535ll * 32) return EF21_ERR_UNSUPPORTED;      // (beyond any device's memory; rows of two million columns)
             s.long_blocks = (unsigned)long_blocks;
             const unsigned blocks = (unsigned)(long_blocks + row_blocks);
-            if (vectors) CU(launch(embedding_sums_kernel<T, O, true>, blocks, ED_SUM_THREADS, 0, st, 1, grad, w.sorted, w.runs, w.partial, out, s));
-            else CU(launch(embedding_sums_kernel<T, O, false>, blocks, ED_SUM_THREADS, 0, st, 1, grad, w.sorted, w.runs, w.partial, out, s));
+            auto sums = [&](auto kernel) -> ef21_status {
+                CU(launch(kernel, blocks, ED_SUM_THREADS, 0, st, 1, grad, w.sorted, w.runs, w.partial, out, s));
+                return EF21_OK;
+            };
+            if (vectors) EF(per_team > 1 ? sums(embedding_sums_kernel<T, O, true, ED_ROWS>) : sums(embedding_sums_kernel<T, O, true, 1>));
+            else EF(per_team > 1 ? sums(embedding_sums_kernel<T, O, false, ED_ROWS>) : sums(embedding_sums_kernel<T, O, false, 1>));
             if (chunks == 0) return EF21_OK;
             s.lanes = 1;                                              // the join's teams: one vector a lane
             while (s.lanes < 32 && s.lanes < columns) s.lanes *= 2;
