@@ -23,6 +23,7 @@ constexpr int ED_THREADS = 256;
 constexpr int ED_SUM_THREADS = 64;          // (a block keeps its place until its slowest team is done)
 constexpr int ED_CHUNK = 32;                // sorted positions that one team adds up
 constexpr int ED_VECS = 2;                  // vectors per lane and row
+constexpr int ED_SINGLES = 2, ED_MANY_SINGLES = 4;   // elements per lane and row where rows are no whole vectors: with eight positions in flight, with four
 constexpr int ED_ROW_VECS = 4;
 constexpr int ED_JOIN_THREADS = 512, ED_SHARES = ED_JOIN_THREADS / 32;
 constexpr int ED_ROWS = 4;                  // rows of the table per team where that leaves enough teams
@@ -238,6 +239,7 @@ struct TableShape {
     int accumulate;
     int lanes, slabs;                       // lanes of a team (a power of two); teams side by side that cover a row
     unsigned long_blocks;                   // blocks that add up chunks of long runs; the others form rows
+    int by_run;                             // rows by their runs: only those that tokens name (zeros have been written, or are not wanted)
 };
 
 template <int VEC> __device__ __forceinline__ void put_floats(float* p, const float (&f)[VEC]) {
@@ -281,24 +283,24 @@ struct Columns {
 };
 
 // Sums over sorted positions [begin, end), in order.  16-bit vectors: two at a time, what is left over alone (registers; whatever else was tried costs the large table 3 %).
-// Others: four or eight (single elements) at a time, the next ones' places looked up meanwhile -- small tables wait for the longest run.
-template <typename T, int VEC>
-__device__ __forceinline__ void add_run(const T* grad, i64 stride, const int2* sorted, int begin, int end, const Columns<VEC, ED_VECS>& c, float (&sum)[ED_VECS][VEC]) {
+// Others: four or eight at a time, the next ones' places looked up meanwhile -- small tables wait for the longest run.
+template <typename T, int VEC, int VECS>
+__device__ __forceinline__ void add_run(const T* grad, i64 stride, const int2* sorted, int begin, int end, const Columns<VEC, VECS>& c, float (&sum)[VECS][VEC]) {
     if constexpr (VEC == 8) {
         auto two_or_one = [&](int i, auto n) {
             constexpr int N = decltype(n)::value;
             const T* g[N];
 #pragma unroll
             for (int p = 0; p < N; ++p) g[p] = grad + (i64)sorted[i + p].y * stride;
-            uint4 u[N][ED_VECS];
+            uint4 u[N][VECS];
 #pragma unroll
             for (int p = 0; p < N; ++p)
 #pragma unroll
-                for (int k = 0; k < ED_VECS; ++k) if (c.in(k)) u[p][k] = load_once(g[p] + c.at(k));
+                for (int k = 0; k < VECS; ++k) if (c.in(k)) u[p][k] = load_once(g[p] + c.at(k));
 #pragma unroll
             for (int p = 0; p < N; ++p)
 #pragma unroll
-                for (int k = 0; k < ED_VECS; ++k) {
+                for (int k = 0; k < VECS; ++k) {
                     float f[Elem<T>::VEC];
                     Elem<T>::unpack(u[p][k], f);
 #pragma unroll
@@ -310,17 +312,17 @@ __device__ __forceinline__ void add_run(const T* grad, i64 stride, const int2* s
         if (i < end) two_or_one(i, std::integral_constant<int, 1>{});
         return;
     }
-    constexpr int N = VEC == 1 ? 8 : 4;
+    constexpr int N = VEC == 1 && VECS == ED_SINGLES ? 8 : 4;
     int at[N];
 #pragma unroll
     for (int p = 0; p < N; ++p) at[p] = begin + p < end ? sorted[begin + p].y : 0;
     for (int i = begin; i < end; i += N) {
         if constexpr (VEC > 1) {
-            uint4 u[N][ED_VECS];
+            uint4 u[N][VECS];
 #pragma unroll
             for (int p = 0; p < N; ++p)
 #pragma unroll
-                for (int k = 0; k < ED_VECS; ++k) {
+                for (int k = 0; k < VECS; ++k) {
                     u[p][k] = make_uint4(0u, 0u, 0u, 0u);
                     if (i + p < end && c.in(k)) u[p][k] = load_once(grad + (i64)at[p] * stride + c.at(k));
                 }
@@ -329,43 +331,43 @@ __device__ __forceinline__ void add_run(const T* grad, i64 stride, const int2* s
 #pragma unroll
             for (int p = 0; p < N; ++p)
 #pragma unroll
-                for (int k = 0; k < ED_VECS; ++k) {
+                for (int k = 0; k < VECS; ++k) {
                     float f[Elem<T>::VEC];
                     Elem<T>::unpack(u[p][k], f);
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) sum[k][e] += f[e];
                 }
         } else {
-            float f[N][ED_VECS];
+            float f[N][VECS];
 #pragma unroll
             for (int p = 0; p < N; ++p)
 #pragma unroll
-                for (int k = 0; k < ED_VECS; ++k) f[p][k] = i + p < end && c.in(k) ? Elem<T>::get(grad[(i64)at[p] * stride + c.at(k)]) : 0.f;
+                for (int k = 0; k < VECS; ++k) f[p][k] = i + p < end && c.in(k) ? Elem<T>::get(grad[(i64)at[p] * stride + c.at(k)]) : 0.f;
 #pragma unroll
             for (int p = 0; p < N; ++p) at[p] = i + N + p < end ? sorted[i + N + p].y : 0;
 #pragma unroll
             for (int p = 0; p < N; ++p)
 #pragma unroll
-                for (int k = 0; k < ED_VECS; ++k) sum[k][0] += f[p][k];
+                for (int k = 0; k < VECS; ++k) sum[k][0] += f[p][k];
         }
     }
 }
 
 // A row's first gradient on its way; zeros where there is none.
-template <typename T, int VEC>
+template <typename T, int VEC, int VECS>
 struct First {
     typedef typename std::conditional<(VEC > 1), uint4, float>::type Raw;
-    Raw raw[ED_VECS];
-    __device__ __forceinline__ void fetch(const T* g, const Columns<VEC, ED_VECS>& c, bool there) {
+    Raw raw[VECS];
+    __device__ __forceinline__ void fetch(const T* g, const Columns<VEC, VECS>& c, bool there) {
 #pragma unroll
-        for (int k = 0; k < ED_VECS; ++k) {
+        for (int k = 0; k < VECS; ++k) {
             if constexpr (VEC > 1) raw[k] = there && c.in(k) ? load_once(g + c.at(k)) : make_uint4(0u, 0u, 0u, 0u);
             else raw[k] = there && c.in(k) ? Elem<T>::get(g[c.at(k)]) : 0.f;
         }
     }
-    __device__ __forceinline__ void take(float (&sum)[ED_VECS][VEC]) const {
+    __device__ __forceinline__ void take(float (&sum)[VECS][VEC]) const {
 #pragma unroll
-        for (int k = 0; k < ED_VECS; ++k) {
+        for (int k = 0; k < VECS; ++k) {
             if constexpr (VEC > 1) Elem<T>::unpack(raw[k], sum[k]);
             else sum[k][0] = raw[k];
         }
@@ -390,21 +392,43 @@ __device__ __forceinline__ void put_row(O* row, const Columns<VEC, VECS>& c, con
     }
 }
 
+// Zeros, 16 KB of a row to a block (a table without gaps is one row).
+template <typename O>
+__global__ void __launch_bounds__(ED_THREADS) embedding_fill_kernel(O* out, i64 slabs, i64 dim, i64 stride) {
+    pdl_wait(out);
+    pdl_trigger();
+    constexpr int VEC = Elem<O>::VEC, SLAB = ED_THREADS * 4;             // vectors
+    const i64 row = blockIdx.x / slabs, slab = blockIdx.x - row * slabs;
+    O* o = out + row * stride;
+    const i64 head = min((i64)row_head(o), dim), vectors = (dim - head) / VEC, tail = head + vectors * VEC;
+    if (slab == 0) {
+        if (threadIdx.x < head) o[threadIdx.x] = Elem<O>::put(0.f);
+        if (tail + threadIdx.x < dim) o[tail + threadIdx.x] = Elem<O>::put(0.f);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const i64 v = slab * SLAB + k * ED_THREADS + threadIdx.x;
+        if (v < vectors) store_vec(o + head + v * VEC, make_uint4(0u, 0u, 0u, 0u));
+    }
+}
+
 // long_blocks of the blocks: chunks of ED_CHUNK sorted positions, the sums of the long runs that they cut.  A run longer than a chunk holds the chunk's first
 // or its last position wherever it meets one: partial[chunk][0] belongs to the first position's run, [1] to the last one's where that is another.
 // The others: rows of the table with no or few positions.
-template <typename T, typename O, bool VECTORS, int ROWS>
+// MANY: there are more teams than the device holds; fewer of them, with more columns and, one after the other, ED_ROWS rows each, take less of everything.
+// Otherwise the launch takes as long as its longest run.
+template <typename T, typename O, bool VECTORS, bool MANY>
 __global__ void __launch_bounds__(ED_SUM_THREADS, 12) embedding_sums_kernel(const T* grad, const int2* sorted, const int2* runs, float* partial, O* out, TableShape s) {
     pdl_wait(grad, sorted, runs, partial, out);
     pdl_trigger();
-    constexpr int VEC = VECTORS ? Elem<T>::VEC : 1;
+    constexpr int VEC = VECTORS ? Elem<T>::VEC : 1, VECS = VECTORS ? ED_VECS : MANY ? ED_MANY_SINGLES : ED_SINGLES, ROWS = MANY ? ED_ROWS : 1;
     const int lane = threadIdx.x & (s.lanes - 1), team = threadIdx.x / s.lanes, teams = ED_SUM_THREADS / s.lanes;
     // blocks of the two kinds take turns: chunks wait for one gradient after the other, rows write
     const unsigned before = (unsigned)((unsigned long long)blockIdx.x * s.long_blocks / gridDim.x);
     const bool chunks = before != (unsigned)((unsigned long long)(blockIdx.x + 1) * s.long_blocks / gridDim.x);
     const i64 item = (i64)(chunks ? before : blockIdx.x - before) * teams + team;
     const i64 at = s.slabs == 1 ? item : item / s.slabs;
-    const Columns<VEC, ED_VECS> c(s, (int)(item - at * s.slabs), lane);
+    const Columns<VEC, VECS> c(s, (int)(item - at * s.slabs), lane);
     if (chunks) {
         const i64 c0 = at * ED_CHUNK, c1 = min(c0 + ED_CHUNK, s.count);
         if (c0 >= s.count) return;
@@ -415,18 +439,31 @@ __global__ void __launch_bounds__(ED_SUM_THREADS, 12) embedding_sums_kernel(cons
             if (key >= s.vocab || (slot == 1 && key == ends[0])) continue;
             const int2 run = runs[key];
             if (run.y - run.x <= ED_CHUNK) continue;
-            float sum[ED_VECS][VEC] = {};
-            add_run<T, VEC>(grad, s.stride, sorted, max(run.x, (int)c0), min(run.y, (int)c1), c, sum);
+            float sum[VECS][VEC] = {};
+            add_run<T, VEC, VECS>(grad, s.stride, sorted, max(run.x, (int)c0), min(run.y, (int)c1), c, sum);
             float* p = partial + (at * 2 + slot) * s.dim;
 #pragma unroll
-            for (int k = 0; k < ED_VECS; ++k) if (c.in(k)) put_floats<VEC>(p + c.at(k), sum[k]);
+            for (int k = 0; k < VECS; ++k) if (c.in(k)) put_floats<VEC>(p + c.at(k), sum[k]);
         }
         return;
     }
     // ROWS rows, one after the other: their runs are looked up together, and a row's first gradient is on its way while the row before it is formed
-    const i64 first = at * ROWS;
-    if (first >= s.vocab) return;
+    const i64 first = s.by_run ? at : at * ROWS;
     int2 run[ROWS], head[ROWS];
+    if (s.by_run) {
+        if (first >= s.count) return;
+        head[0] = sorted[first];
+        if (head[0].x >= s.vocab || (first > 0 && sorted[first - 1].x == head[0].x)) return;             // (no run begins here)
+        run[0] = runs[head[0].x];
+        if (run[0].y - run[0].x > ED_CHUNK) return;
+        First<T, VEC, VECS> one;
+        float sum[VECS][VEC];
+        one.fetch(grad + (i64)head[0].y * s.stride, c, true);
+        one.take(sum);
+        if (run[0].y - run[0].x > 1) add_run<T, VEC, VECS>(grad, s.stride, sorted, run[0].x + 1, run[0].y, c, sum);
+        put_row<O, VEC, VECS>(out + (i64)head[0].x * s.out_stride, c, sum, s);
+        return;
+    }
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
         run[r] = first + r < s.vocab ? runs[first + r] : make_int2(-1, -1);
@@ -434,20 +471,20 @@ __global__ void __launch_bounds__(ED_SUM_THREADS, 12) embedding_sums_kernel(cons
     }
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) if (head[r].x != first + r) run[r] = make_int2(0, 0);          // no such token
-    First<T, VEC> next;
+    First<T, VEC, VECS> next;
     next.fetch(grad + (i64)head[0].y * s.stride, c, run[0].y > run[0].x && run[0].y - run[0].x <= ED_CHUNK);
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
         const int n = run[r].y - run[r].x;
-        float sum[ED_VECS][VEC];
+        float sum[VECS][VEC];
         next.take(sum);
         if (r + 1 < ROWS) {
             const int m = run[(r + 1) % ROWS].y - run[(r + 1) % ROWS].x;
             next.fetch(grad + (i64)head[(r + 1) % ROWS].y * s.stride, c, m > 0 && m <= ED_CHUNK);
         }
         if (first + r >= s.vocab || n > ED_CHUNK || (n == 0 && s.accumulate)) continue;
-        if (n > 1) add_run<T, VEC>(grad, s.stride, sorted, run[r].x + 1, run[r].y, c, sum);
-        put_row<O, VEC>(out + (first + r) * s.out_stride, c, sum, s);
+        if (n > 1) add_run<T, VEC, VECS>(grad, s.stride, sorted, run[r].x + 1, run[r].y, c, sum);
+        put_row<O, VEC, VECS>(out + (first + r) * s.out_stride, c, sum, s);
     }
 }
 
@@ -501,7 +538,7 @@ __global__ void __launch_bounds__(ED_JOIN_THREADS) embedding_join_kernel(const i
         if (n <= ED_SHARES) {
             float sum[1][VEC] = {};
             add_partials(partial, chunk, chunk + n, run.x > chunk * ED_CHUNK ? chunk : -1, c, sum);
-            put_row<O, VEC>(out + (i64)keys[team] * s.out_stride, c, sum, s);
+            put_row<O, VEC, 1>(out + (i64)keys[team] * s.out_stride, c, sum, s);
         }
     }
     if (!longest) return;
@@ -522,7 +559,7 @@ __global__ void __launch_bounds__(ED_JOIN_THREADS) embedding_join_kernel(const i
             for (int t = 1; t < min(ED_SHARES, n); ++t)
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) sum[0][e] += mine[(size_t)t * s.lanes * VEC + e * s.lanes];
-            put_row<O, VEC>(out + (i64)keys[w] * s.out_stride, c, sum, s);
+            put_row<O, VEC, 1>(out + (i64)keys[w] * s.out_stride, c, sum, s);
         }
         __syncthreads();
     }

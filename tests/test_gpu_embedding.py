@@ -101,6 +101,23 @@ def test_adding_to_a_gradient(B, dtype, dim):
         assert torch.equal(table[:, :dim], B.embedding_grad(grad, tokens, 120, scale=0.5, dtype=out_dtype)) and torch.equal(table[:, dim:], before[:, dim:])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("count,vocab,dim", [(4, 98621, 61), (3000, 70000, 64), (900, 20000, 333), (70000, 300000, 16), (40000, 12000, 1001), (1, 5, 2000003)])
+def test_large_tables(B, dtype, count, vocab, dim):
+    """Tables that are cleared first, and rows formed four to a team; with and without gaps between the rows, which stay as they are."""
+    g = generator(count)
+    grad = torch.randn(count, dim, device="cuda", generator=g).to(dtype)
+    tokens = (vocab ** torch.rand(count, device="cuda", generator=g, dtype=torch.float64)).long().clamp_(max=vocab) - 1
+    if count > 1:
+        tokens[::9] = vocab
+        tokens[1::50] = vocab - 1
+    want = check_grad(B, grad, tokens, vocab, scale=0.5, dtype=torch.float32)
+    table = torch.full((vocab, dim + 3), 7.0, device="cuda")
+    B.embedding_grad(grad, tokens, vocab, scale=0.5, out=table[:, 1:dim + 1])
+    assert torch.equal(table[:, 1:dim + 1], want) and bool((table[:, 0] == 7).all()) and bool((table[:, dim + 1:] == 7).all())
+    check_grad(B, grad, tokens, vocab)
+
+
 def test_views_and_empty(B):
     grad = torch.randn(50, 24, device="cuda", dtype=torch.bfloat16)
     tokens = torch.randint(0, 9, (50,), device="cuda")
