@@ -80,14 +80,15 @@ __global__ void __launch_bounds__(BL_COUNT_THREADS) balance_count_kernel(const v
     if (threadIdx.x == 0 && tokens) atomicAdd(&work->tokens, tokens);
 }
 
-// A team of s.lanes lanes takes ROWS rows at a time; lane l has PER vectors of VEC columns, lanes side by side -- of whole vectors where the number of columns
-// is a multiple of them, however the rows are aligned: the order of the additions goes by the number of columns alone.
+// A team of s.lanes lanes takes ROWS rows at a time; lane l has PER vectors of VEC columns, lanes side by side, the last vector of a row perhaps not full.  Rows that are
+// no whole aligned vectors are read and written element by element, in the same order of lanes and additions.
 // LANES: 32 or 16, or 0 where s.lanes may be fewer.
-template <typename T, int VEC, int PER, int ROWS, int LANES>
-__global__ void __launch_bounds__(BL_THREADS, PER * VEC <= 16 ? 3 : 1) balance_kernel(const T* logits, const void* choices, const unsigned char* mask, int* counts, const BalanceWork* work, T* grad, float* partial,
+template <typename T, int PER, int ROWS, int LANES>
+__global__ void __launch_bounds__(BL_THREADS, PER * Elem<T>::VEC <= 16 ? 3 : 1) balance_kernel(const T* logits, const void* choices, const unsigned char* mask, int* counts, const BalanceWork* work, T* grad, float* partial,
                                                              float* probs, float* loss, BalanceShape s) {
     pdl_wait(logits, choices, mask, counts, work, grad, partial, probs, loss);
     pdl_trigger();
+    constexpr int VEC = Elem<T>::VEC;
     __shared__ float column[BL_MAX_EXPERTS];
     __shared__ int here[BL_MAX_EXPERTS];
     extern __shared__ float of_warp[];                                // [warps][E]
@@ -107,7 +108,7 @@ __global__ void __launch_bounds__(BL_THREADS, PER * VEC <= 16 ? 3 : 1) balance_k
     }
     const double N = (double)(s.one ? seen : work->tokens), KN = N * s.chosen;
     auto column_of = [&](int i) { return (lane + i / VEC * lanes) * VEC + i % VEC; };
-    constexpr int PAIRS = VEC > 1 ? PER * VEC / 2 : PER;
+    constexpr int PAIRS = PER * VEC / 2;
     __shared__ float about_mean[BL_MAX_EXPERTS];
     for (int e = tid; e < E; e += BL_THREADS) about_mean[e] = N > 0.0 ? (float)(((double)(s.one ? here[e] : counts[e]) * E - KN) / (KN * E)) : 0.f;
     __syncthreads();
@@ -115,13 +116,12 @@ __global__ void __launch_bounds__(BL_THREADS, PER * VEC <= 16 ? 3 : 1) balance_k
     Two apart[PAIRS], sum[PAIRS];
 #pragma unroll
     for (int i = 0; i < PAIRS; ++i) {
-        apart[i] = VEC > 1 ? two(share(column_of(2 * i)), share(column_of(2 * i + 1))) : two(share(column_of(i)), 0.f);
+        apart[i] = two(share(column_of(2 * i)), share(column_of(2 * i + 1)));
         sum[i] = two(0.f);
     }
     const float factor = N > 0.0 ? (float)(s.weight * E / N) : 0.f;
     const i64 step = (i64)gridDim.x * groups;
-    uint4 raw[ROWS][VEC > 1 ? PER : 1];
-    float single[ROWS][VEC > 1 ? 1 : PER];
+    uint4 raw[ROWS][PER];
     bool counts_in[ROWS];
     auto fetch = [&](i64 row0) {
 #pragma unroll
@@ -133,22 +133,17 @@ __global__ void __launch_bounds__(BL_THREADS, PER * VEC <= 16 ? 3 : 1) balance_k
             for (int i = 0; i < PER; ++i) {
                 const int at = (lane + i * lanes) * VEC;
                 if (row >= s.rows || at >= E) continue;
-                if constexpr (VEC == 1) {
-                    single[r][i] = Elem<T>::get(x[at]);
-                } else if (s.whole_in) {
-                    raw[r][i] = load_once(x + at);
-                } else {
-                    float v[VEC];
+                if (s.whole_in) { raw[r][i] = load_once(x + at); continue; }
+                float v[VEC];
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) v[e] = Elem<T>::get(x[at + e]);
-                    raw[r][i] = Elem<T>::pack(v);
-                }
+                for (int e = 0; e < VEC; ++e) v[e] = at + e < E ? Elem<T>::get(x[at + e]) : -INFINITY;
+                raw[r][i] = Elem<T>::pack(v);
             }
         }
     };
     fetch((i64)blockIdx.x * groups + group);
     for (i64 row0 = (i64)blockIdx.x * groups + group; row0 - group < s.rows; row0 += step * ROWS) {     // (whole warps: the shuffles need every lane)
-        // (fp32 pairs: one instruction for two columns; a single column has a pair to itself)
+        // (fp32 pairs: one instruction for two columns)
         Two f[ROWS][PAIRS];
         float top[ROWS], total[ROWS], mean[ROWS];
         bool keep[ROWS];
@@ -159,20 +154,13 @@ __global__ void __launch_bounds__(BL_THREADS, PER * VEC <= 16 ? 3 : 1) balance_k
             top[r] = -INFINITY;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const bool none = !keep[r] || (lane + i * lanes) * VEC >= E;
-                if constexpr (VEC == 1) {
-                    if (none) single[r][i] = -INFINITY;
-                    top[r] = fmaxf(top[r], single[r][i]);
-                    f[r][i] = two(single[r][i], -INFINITY);
-                } else {
-                    constexpr unsigned nothing = Elem<T>::NEG_INF;
-                    if (none) raw[r][i] = make_uint4(nothing, nothing, nothing, nothing);
-                    top[r] = fmaxf(top[r], Elem<T>::top(raw[r][i]));
-                    float v[VEC];
-                    Elem<T>::unpack(raw[r][i], v);
+                constexpr unsigned nothing = Elem<T>::NEG_INF;
+                if (!keep[r] || (lane + i * lanes) * VEC >= E) raw[r][i] = make_uint4(nothing, nothing, nothing, nothing);
+                top[r] = fmaxf(top[r], Elem<T>::top(raw[r][i]));
+                float v[VEC];
+                Elem<T>::unpack(raw[r][i], v);
 #pragma unroll
-                    for (int e = 0; e < VEC; e += 2) f[r][(i * VEC + e) / 2] = two(v[e], v[(e + 1) % VEC]);
-                }
+                for (int e = 0; e < VEC; e += 2) f[r][(i * VEC + e) / 2] = two(v[e], v[e + 1]);
             }
         }
         fetch(row0 + step * ROWS);                                           // (on their way while these rows are worked on)
@@ -228,18 +216,12 @@ __global__ void __launch_bounds__(BL_THREADS, PER * VEC <= 16 ? 3 : 1) balance_k
             for (int i = 0; i < PER; ++i) {
                 const int at = (lane + i * lanes) * VEC;
                 if (at >= E) continue;
-                if constexpr (VEC == 1) {
-                    float a, b;
-                    split(f[r][i], a, b);
-                    g[at] = Elem<T>::put(a);
-                } else {
-                    float v[VEC];
+                float v[VEC];
 #pragma unroll
-                    for (int e = 0; e < VEC; e += 2) split(f[r][(i * VEC + e) / 2], v[e], v[(e + 1) % VEC]);
-                    if (s.whole_out) { store_vec(g + at, Elem<T>::pack(v)); continue; }
+                for (int e = 0; e < VEC; e += 2) split(f[r][(i * VEC + e) / 2], v[e], v[e + 1]);
+                if (s.whole_out) { store_vec(g + at, Elem<T>::pack(v)); continue; }
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) g[at + e] = Elem<T>::put(v[e]);
-                }
+                for (int e = 0; e < VEC; ++e) if (at + e < E) g[at + e] = Elem<T>::put(v[e]);
             }
         }
     }
@@ -254,9 +236,9 @@ __global__ void __launch_bounds__(BL_THREADS, PER * VEC <= 16 ? 3 : 1) balance_k
         for (int i = 0; i < PAIRS; ++i) {
             float a, b;
             split(sum[i], a, b);
-            const int e = column_of(VEC > 1 ? 2 * i : i);
+            const int e = column_of(2 * i);
             if (e < E) mine[e] = a;
-            if (VEC > 1 && e + 1 < E) mine[e + 1] = b;
+            if (e + 1 < E) mine[e + 1] = b;
         }
     }
     __syncthreads();

@@ -82,6 +82,42 @@ __device__ __forceinline__ uint4 load_once(const void* p) {
 }
 __device__ __forceinline__ void store_vec(void* p, uint4 v) { *reinterpret_cast<uint4*>(p) = v; }
 
+// N times 16 bytes from any address: the lanes of a warp, all of them, take consecutive 16 bytes (in: this lane does; last: nobody behind it does), N * 32 of these
+// `step` bytes apart.  Two aligned loads would do for each, of which the second is the next lane's first.  What is read beside the bytes wanted lies in the same
+// aligned 16 bytes as one of them.
+template <int N>
+__device__ __forceinline__ void load_unaligned(const void* const (&p)[N], const bool (&in)[N], const bool (&last)[N], uint4 (&out)[N]) {
+    const int lane = threadIdx.x & 31;
+    uint4 own[N], more[N];
+    bool extra[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p[k]);
+        own[k] = more[k] = make_uint4(0u, 0u, 0u, 0u);
+        extra[k] = in[k] && (last[k] || lane == 31) && (at & 15u) != 0;
+        if (in[k]) own[k] = load_once(reinterpret_cast<const void*>(at & ~(uintptr_t)15));
+        if (extra[k]) more[k] = load_once(reinterpret_cast<const void*>((at & ~(uintptr_t)15) + 16));
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        unsigned w[8] = {own[k].x, own[k].y, own[k].z, own[k].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[4 + i] = __shfl_down_sync(0xffffffffu, w[i], 1);
+        if (extra[k]) { w[4] = more[k].x; w[5] = more[k].y; w[6] = more[k].z; w[7] = more[k].w; }
+        const unsigned by = (unsigned)(reinterpret_cast<uintptr_t>(p[k]) & 15u);
+        if (by & 8u) {
+#pragma unroll
+            for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+        }
+        if (by & 4u) {
+#pragma unroll
+            for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+        }
+        const unsigned bits = (by & 3u) * 8u;
+        out[k] = make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
+    }
+}
+
 // Indices are 32 or 64 bits wide.
 __device__ __forceinline__ i64 index_at(const void* p, int wide, i64 i) {
     return wide ? static_cast<const long long*>(p)[i] : (i64)static_cast<const int*>(p)[i];

@@ -24,7 +24,7 @@ constexpr int ED_SUM_THREADS = 64;          // (a block keeps its place until it
 constexpr int ED_CHUNK = 32;                // sorted positions that one team adds up
 constexpr int ED_VECS = 2;                  // vectors per lane and row
 constexpr int ED_SINGLES = 2, ED_MANY_SINGLES = 4;   // elements per lane and row where rows are no whole vectors: with eight positions in flight, with four
-constexpr int ED_ROW_VECS = 4;
+constexpr int ED_ROW_VECS = 4, ED_SHORT = 512;
 constexpr int ED_JOIN_THREADS = 512, ED_SHARES = ED_JOIN_THREADS / 32;
 constexpr int ED_ROWS = 4;                  // rows of the table per team where that leaves enough teams
 constexpr int ED_RANK_TOKENS = 4096;
@@ -33,43 +33,67 @@ constexpr int RX_THREADS = 1024, RX_ITEMS = 1, RX_TILE = RX_THREADS * RX_ITEMS, 
 
 // ---- lookup -------------------------------------------------------------------------------------------------------------------------------
 
-// A warp takes ED_ROW_VECS times 32 vectors (VECTORS: 16 bytes, rows are whole numbers of them and aligned; else elements) of one row.
-template <typename T, bool VECTORS>
+// A warp takes ED_ROW_VECS times 32 vectors of one row.  ALIGNED: rows of the table and of the output are whole aligned vectors; otherwise vectors are those of the output, and
+// the first and the last warp of a row write the elements around them.
+template <typename T, bool ALIGNED>
 __global__ void __launch_bounds__(ED_THREADS) embedding_kernel(const T* weight, const void* tokens, T* out, i64 items, int slabs, i64 vocab, i64 dim, i64 stride, int wide, float scale) {
     pdl_wait(weight, tokens, out);
     pdl_trigger();
-    constexpr int VEC = VECTORS ? Elem<T>::VEC : 1;
+    constexpr int VEC = Elem<T>::VEC;
     const i64 item = (i64)blockIdx.x * (ED_THREADS / 32) + (threadIdx.x >> 5);
     if (item >= items) return;
+    const int lane = threadIdx.x & 31;
     const i64 t = slabs == 1 ? item : item / slabs;
-    const i64 first = (item - t * slabs) * (32 * ED_ROW_VECS * VEC) + (threadIdx.x & 31) * VEC;
+    const int slab = (int)(item - t * slabs);
     const i64 v = index_at(tokens, wide, t);
     const bool in = v >= 0 && v < vocab;
     const T* row = weight + (in ? v : 0) * stride;
     T* o = out + t * dim;
-    if (VECTORS) {
-        uint4 u[ED_ROW_VECS];
+    const i64 head = ALIGNED ? 0 : min((i64)row_head(o), dim), vectors = (dim - head) / VEC, first = (i64)slab * (32 * ED_ROW_VECS) + lane;
+    uint4 u[ED_ROW_VECS];
+    if (ALIGNED) {
 #pragma unroll
-        for (int k = 0; k < ED_ROW_VECS; ++k) {
-            const i64 j = first + k * 32 * VEC;
-            u[k] = in && j < dim ? *reinterpret_cast<const uint4*>(row + j) : make_uint4(0u, 0u, 0u, 0u);
-        }
-#pragma unroll
-        for (int k = 0; k < ED_ROW_VECS; ++k) {
-            const i64 j = first + k * 32 * VEC;
-            float f[Elem<T>::VEC];
-            Elem<T>::unpack(u[k], f);
-#pragma unroll
-            for (int e = 0; e < Elem<T>::VEC; ++e) f[e] = in ? f[e] * scale : 0.f;
-            if (j < dim) store_vec(o + j, Elem<T>::pack(f));
-        }
+        for (int k = 0; k < ED_ROW_VECS; ++k)
+            u[k] = in && first + k * 32 < vectors ? *reinterpret_cast<const uint4*>(row + (first + k * 32) * VEC) : make_uint4(0u, 0u, 0u, 0u);
     } else {
-        float f[ED_ROW_VECS];
+        const void* p[ED_ROW_VECS];
+        bool there[ED_ROW_VECS], last[ED_ROW_VECS];
 #pragma unroll
-        for (int k = 0; k < ED_ROW_VECS; ++k) f[k] = in && first + k * 32 < dim ? Elem<T>::get(row[first + k * 32]) : 0.f;
-#pragma unroll
-        for (int k = 0; k < ED_ROW_VECS; ++k) if (first + k * 32 < dim) o[first + k * 32] = Elem<T>::put(in ? f[k] * scale : 0.f);
+        for (int k = 0; k < ED_ROW_VECS; ++k) {
+            p[k] = row + head + (first + k * 32) * VEC;
+            there[k] = in && first + k * 32 < vectors; last[k] = first + k * 32 + 1 == vectors;
+        }
+        load_unaligned<ED_ROW_VECS>(p, there, last, u);
+        auto one = [&](i64 j) { o[j] = Elem<T>::put(in ? Elem<T>::get(row[j]) * scale : 0.f); };
+        if (slab == 0 && lane < head) one(lane);
+        if (slab == slabs - 1 && head + vectors * VEC + lane < dim) one(head + vectors * VEC + lane);
     }
+#pragma unroll
+    for (int k = 0; k < ED_ROW_VECS; ++k) {
+        float f[VEC];
+        Elem<T>::unpack(u[k], f);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) f[e] = in ? f[e] * scale : 0.f;
+        if (first + k * 32 < vectors) store_vec(o + head + (first + k * 32) * VEC, Elem<T>::pack(f));
+    }
+}
+
+// Short rows that are no whole aligned vectors (up to ED_SHORT elements): a warp has a row.
+template <typename T>
+__global__ void __launch_bounds__(ED_THREADS) embedding_short_kernel(const T* weight, const void* tokens, T* out, i64 count, i64 vocab, i64 dim, i64 stride, int wide, float scale) {
+    pdl_wait(weight, tokens, out);
+    pdl_trigger();
+    const int lane = threadIdx.x & 31;
+    const i64 t = (i64)blockIdx.x * (ED_THREADS / 32) + (threadIdx.x >> 5);
+    if (t >= count) return;
+    const i64 v = index_at(tokens, wide, t);
+    const bool in = v >= 0 && v < vocab;
+    const T* row = weight + (in ? v : 0) * stride;
+    float f[ED_SHORT / 32];
+#pragma unroll
+    for (int k = 0; k < ED_SHORT / 32; ++k) f[k] = in && lane + k * 32 < dim ? Elem<T>::get(row[lane + k * 32]) : 0.f;
+#pragma unroll
+    for (int k = 0; k < ED_SHORT / 32; ++k) if (lane + k * 32 < dim) out[t * dim + lane + k * 32] = Elem<T>::put(in ? f[k] * scale : 0.f);
 }
 
 // ---- sorting positions by token -------------------------------------------------------------------------------------------------------------

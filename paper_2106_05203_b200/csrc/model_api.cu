@@ -335,11 +335,10 @@ ef21_status ef21_balance_loss(const void* logits_dev, int32_t dtype, int64_t row
         constexpr int V = Elem<T>::VEC;
         const T* logits = static_cast<const T*>(logits_dev);
         T* grad = static_cast<T*>(grad_out_dev);
-        const bool vectors = experts % V == 0;
-        const i64 columns = vectors ? experts / V : experts;
-        BalanceShape s{rows, (int)experts, (int)chosen, index_type, logits_stride, choices_stride, weight, 1, 0, aligned(logits, 16) && logits_stride % V == 0, aligned(grad, 16)};
+        const i64 columns = ceil_div(experts, V);
+        BalanceShape s{rows, (int)experts, (int)chosen, index_type, logits_stride, choices_stride, weight, 1, 0, experts % V == 0 && aligned(logits, 16) && logits_stride % V == 0, experts % V == 0 && aligned(grad, 16)};
         // two vectors a lane where there are enough: a row's shuffles, division and addresses are shared by fewer lanes
-        while (s.lanes < 32 && s.lanes * (vectors ? 2 : 1) < columns) s.lanes *= 2;
+        while (s.lanes < 32 && s.lanes * 2 < columns) s.lanes *= 2;
         s.one = rows * chosen <= BL_ONE_CHOICES && rows * experts <= BL_ONE_LOGITS;
         const unsigned blocks = grid_of(rows, BL_THREADS / s.lanes, s.one ? BL_CLUSTER : BL_MAX_BLOCKS);
         if (!s.one) {
@@ -351,16 +350,9 @@ ef21_status ef21_balance_loss(const void* logits_dev, int32_t dtype, int64_t row
             return EF21_OK;
         };
         // rows in flight per team: 16 values per lane or more
-        const bool full = s.lanes == 32;
-        if (vectors) {
-            if (columns <= 64) EF(full ? run(balance_kernel<T, V, 2, 8 / V, 32>) : s.lanes == 16 ? run(balance_kernel<T, V, 2, 8 / V, 16>) : run(balance_kernel<T, V, 2, 8 / V, 0>));
-            else if (columns <= 128) EF(run(balance_kernel<T, V, 4, 1, 32>));
-            else if constexpr (V == 4) EF(run(balance_kernel<T, V, 8, 1, 32>));
-        } else {
-            if (columns <= 32) EF(full ? run(balance_kernel<T, 1, 1, 4, 32>) : run(balance_kernel<T, 1, 1, 4, 0>));
-            else if (columns <= 128) EF(run(balance_kernel<T, 1, 4, 4, 32>));
-            else EF(run(balance_kernel<T, 1, 32, 1, 32>));
-        }
+        if (columns <= 64) EF(s.lanes == 32 ? run(balance_kernel<T, 2, 8 / V, 32>) : s.lanes == 16 ? run(balance_kernel<T, 2, 8 / V, 16>) : run(balance_kernel<T, 2, 8 / V, 0>));
+        else if (columns <= 128) EF(run(balance_kernel<T, 4, 1, 32>));
+        else if constexpr (V == 4) EF(run(balance_kernel<T, 8, 1, 32>));
         if (!s.one) CU(launch(balance_finish_kernel, (unsigned)ceil_div(experts, BL_FINISH_COLUMNS), BL_FINISH_COLUMNS * BL_FINISH_GROUPS, 0, st, 1, w.partial, counts_out_dev, w.work, w.part,
                               probs_out_dev, loss_out_dev, (int)blocks, (int)experts, (int)chosen, weight));
         return EF21_OK;
@@ -379,7 +371,11 @@ ef21_status ef21_embedding(const void* weight_dev, int32_t dtype, int64_t vocab,
         T* out = static_cast<T*>(out_dev);
         cudaStream_t st = stream_of(cuda_stream);
         const bool vectors = aligned(weight, 16) && aligned(out, 16) && dim % VEC == 0 && weight_stride % VEC == 0;
-        const i64 slabs = ceil_div(dim, (i64)32 * ED_ROW_VECS * (vectors ? VEC : 1)), items = count * slabs;
+        if (!vectors && dim <= ED_SHORT) {                            // (30,000 rows of 63 bf16: 6 us, 16 by vectors of the output)
+            CU(launch(embedding_short_kernel<T>, (unsigned)ceil_div(count, ED_THREADS / 32), ED_THREADS, 0, st, 1, weight, tokens_dev, out, count, vocab, dim, weight_stride, index_type, scale));
+            return EF21_OK;
+        }
+        const i64 slabs = ceil_div(dim, (i64)32 * ED_ROW_VECS * VEC), items = count * slabs;
         if (ceil_div(items, ED_THREADS / 32) > MOST) return EF21_ERR_UNSUPPORTED;        // (1 TB of output and more)
         const unsigned blocks = (unsigned)ceil_div(items, ED_THREADS / 32);
         if (vectors) CU(launch(embedding_kernel<T, true>, blocks, ED_THREADS, 0, st, 1, weight, tokens_dev, out, items, (int)slabs, vocab, dim, weight_stride, index_type, scale));

@@ -258,15 +258,40 @@ __device__ __forceinline__ void grad_span(const T* x, T* out, i64 begin, i64 end
         const float p = r.a * exp2_fast(fmaf(f, r.scale, -r.lse) * LOG2E);
         return j == r.target ? r.a - p : -p;
     };
+    auto gradient = [&](uint4 u, i64 j) {                              // of the vector at j
+        float f[VEC];
+        Elem<T>::unpack(u, f);
+        const bool named = r.target >= j && r.target < j + VEC;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) f[e] = -r.a * exp2_fast(fmaf(f[e], r.scale, -r.lse) * LOG2E);
+        if (named) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) if (j + e == r.target) f[e] += r.a;
+        }
+        return Elem<T>::pack(f);
+    };
     auto one = [&](i64 j) { out[j] = Elem<T>::put(r.zero ? 0.f : value(Elem<T>::get(x[j]), j)); };
-    if (row_head(x + begin) != row_head(out + begin)) {       // rows of different alignment: element by element
-        for (i64 j = begin + tid; j < end; j += threads) one(j);
-        return;
-    }
-    const i64 head = min((i64)row_head(x + begin), end - begin), vectors = (end - begin - head) / VEC, tail = end - begin - head - vectors * VEC;
+    const i64 head = min((i64)row_head(out + begin), end - begin), vectors = (end - begin - head) / VEC, tail = end - begin - head - vectors * VEC;
     if (tid < head) one(begin + tid);
     if (tid < tail) one(end - tail + tid);
     const i64 body = begin + head;
+    if (row_head(x + begin) != row_head(out + begin) && !r.zero) {       // logits of another alignment
+        constexpr int N = 2;
+        for (i64 v = tid; v - (tid & 31) < vectors; v += (i64)threads * N) {
+            const void* p[N];
+            bool in[N], last[N];
+            uint4 u[N];
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const i64 at = v + (i64)k * threads;
+                p[k] = x + body + at * VEC; in[k] = at < vectors; last[k] = at + 1 == vectors;
+            }
+            load_unaligned<N>(p, in, last, u);
+#pragma unroll
+            for (int k = 0; k < N; ++k) if (in[k]) store_vec(out + body + (v + (i64)k * threads) * VEC, gradient(u[k], body + (v + (i64)k * threads) * VEC));
+        }
+        return;
+    }
     for (i64 v = tid; v < vectors; v += (i64)threads * LG_UNROLL) {
         uint4 u[LG_UNROLL];
 #pragma unroll
@@ -279,16 +304,7 @@ __device__ __forceinline__ void grad_span(const T* x, T* out, i64 begin, i64 end
             const i64 at = v + (i64)k * threads, j = body + at * VEC;
             if (at >= vectors) break;
             if (r.zero) { store_vec(out + j, make_uint4(0u, 0u, 0u, 0u)); continue; }
-            float f[VEC];
-            Elem<T>::unpack(u[k], f);
-            const bool named = r.target >= j && r.target < j + VEC;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) f[e] = -r.a * exp2_fast(fmaf(f[e], r.scale, -r.lse) * LOG2E);
-            if (named) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) if (j + e == r.target) f[e] += r.a;
-            }
-            store_vec(out + j, Elem<T>::pack(f));
+            store_vec(out + j, gradient(u[k], j));
         }
     }
 }
