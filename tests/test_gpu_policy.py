@@ -114,6 +114,22 @@ def test_small_and_large_differences(B):
     assert abs(float(got.terms[0]) + 1.2 * 3.5 / 4) < 1e-6 and not bool(got.grad.any())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("length", [16, 19])
+def test_tokens_that_the_reference_rules_out(B, dtype, length):
+    """delta far below 0, down to the type's lowest value and -inf: the KL term grows without bound, its slope is -1.  d = 0 and A = 0, so the gradient is the
+    slope's alone, weight (1 - exp(delta)) / tokens: exact to the roundings of the weight, the product and the result."""
+    lp = torch.full((2, length), -1.0, device="cuda", dtype=dtype)
+    zero = torch.zeros_like(lp)
+    for low in (-30.0, -3000.0, -65504.0, torch.finfo(dtype).min, -float("inf")):
+        ref = torch.full_like(lp, -1.0)
+        ref[0, 3] = low; ref[1, length - 1] = low
+        got = B.policy_loss(lp, lp, zero, ref_logps=ref, kl_weight=0.5)
+        want = torch.zeros(2, length, dtype=torch.float64, device="cuda")
+        want[0, 3] = want[1, length - 1] = 0.5 * -torch.expm1(torch.tensor(low + 1.0, dtype=torch.float64)) / (2 * length)
+        assert_within(got.grad, want, rounding(want, dtype) + 6 * EPS * want.abs(), f"gradient at {low}")
+
+
 def test_gradient_against_differences(B):
     """Central differences of the 64-bit definition, h = 1e-5, at tokens away from the borders (no third derivative over 10 / 60 tokens): below 1e-10; the kernel 2^-18."""
     lp, old, adv, mask, ref = inputs(3, 20, torch.float32, 8)
