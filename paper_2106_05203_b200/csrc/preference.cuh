@@ -116,7 +116,14 @@ __global__ void __launch_bounds__(PF_THREADS) preference_kernel(const T* logps, 
                 Elem<T>::unpack(y[side], fy);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) some += (w[side] >> (8 * e) & 255u) != 0 ? fx[e] - fy[e] : 0.f;
-                sum[side] += (double)some;
+                if (!(fabsf(some) <= 3.4028234e38f)) {                // (lowest values of a mask: their sum is beyond 32 bits, each is not)
+                    double exact = 0.0;
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) exact += (w[side] >> (8 * e) & 255u) != 0 ? (double)fx[e] - (double)fy[e] : 0.0;
+                    sum[side] += exact;
+                } else {
+                    sum[side] += (double)some;
+                }
             }
         } else {
 #pragma unroll
@@ -153,11 +160,12 @@ __global__ void __launch_bounds__(PF_THREADS) preference_kernel(const T* logps, 
     float slope = 0.f;
     if (lane == 0 && there) {
         const double z = s.beta * (sum[0] - sum[1]), e = exp(-fabs(z));
-        const double low = log1p(e) + fmax(-z, 0.0);                           // -log sigma(z); -log sigma(-z) is larger by z
+        const double low = log1p(e);                                           // -log sigma(|z|); -log sigma(-|z|) is larger by |z|
         const double sigma = (z >= 0.0 ? e : 1.0) / (1.0 + e);                 // of -z
         slope = (float)(s.beta / s.norm * (sigma - s.smoothing));
         if (part == 0) {
-            loss = s.smoothing == 0.0 ? low : low + s.smoothing * z;
+            const double share = z < 0.0 ? 1.0 - s.smoothing : s.smoothing;
+            loss = share == 0.0 ? low : low + share * fabs(z);
             rewards[p] = (float)(s.beta * sum[0]);
             rewards[p + s.pairs] = (float)(s.beta * sum[1]);
         }

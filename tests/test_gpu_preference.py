@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from model_util import TYPES, assert_within, generator, preference64, rounding
+from model_util import EPS, TYPES, assert_within, generator, preference64, rounding
 
 pytestmark = pytest.mark.gpu
 
@@ -88,6 +88,31 @@ def test_gradient_against_differences(B):
             x = lp.double(); x[r, t] += sign * 1e-4
             at.append(preference64(x, ref, mask, 0.5, 0.1)[0][0])
         assert abs(float((at[0] - at[1]) / 2e-4 - got.grad[r, t].double())) < 1e-9 + 0.5 * 2.0 ** -20
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("length", [12, 300, 2051])
+def test_tokens_that_are_ruled_out(B, dtype, length):
+    """Log-probabilities of the type's lowest value and of -inf, in one vector and in several: the loss is the formula's (a margin of -+inf: infinite where its term has a
+    weight, 0 where not), the slope beta / P times 1 - eps or -eps, exact to its roundings, as the sigma is 0 or 1."""
+    pairs, beta, least = 3, 0.1, torch.finfo(dtype).min
+    for low in (least, -float("inf")):
+        for side, eps in ((0, 0.0), (0, 0.1), (1, 0.0), (1, 0.1), (0, 1.0), (1, 1.0)):
+            lp = torch.full((2 * pairs, length), -1.0, device="cuda", dtype=dtype)
+            lp[side * pairs, 8:12] = low
+            got = B.preference_loss(lp, beta=beta, smoothing=eps)
+            d = lp.double().sum(1)
+            z = beta * (d[:pairs] - d[pairs:])
+            term = lambda weight, v: weight * torch.nn.functional.softplus(v) if weight else torch.zeros_like(v)
+            each = term(1 - eps, -z) + term(eps, z)
+            # sums of magnitudes: those of at most `length` ones, and up to eight added in 32 bits
+            off = 12 * EPS * (each[torch.isfinite(each)].abs().sum() + beta * length)
+            assert_within(got.loss, each.sum() / pairs, off, "loss")
+            assert_within(got.rewards, beta * d, 12 * EPS * (beta * d).abs(), "rewards")
+            slope = beta / pairs * (torch.sigmoid(-z) - eps)
+            want = torch.cat([-slope, slope])[:, None].expand(2 * pairs, length)
+            tol = rounding(want, dtype) + 4 * EPS * want.abs()
+            assert_within(got.grad, want, tol, "gradient")
 
 
 def test_repeated_captured_and_on_another_stream(B):
