@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(BL_THREADS, PER * Elem<T>::VEC <= 16 ? 3 : 1) 
         for (int r = 0; r < ROWS; ++r) {
             float base = top[r] == -INFINITY ? 0.f : top[r];                 // (a row of -inf only, or left out: all 0)
             const Two exponent = two(LOG2E);
-            if (base < -1e38f) {                                             // (a mask of the type's lowest value: it times log2 e would overflow)
+            if (fabsf(base) > 1e38f) {                                       // (a mask of the type's lowest value, a choice forced by its largest: it times log2 e would overflow)
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) f[r][i] = add2(f[r][i], two(-base));
                 base = 0.f;

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from model_util import TYPES, assert_within, balance64, generator, rounding
+from model_util import EPS, TYPES, assert_within, balance64, generator, rounding
 
 pytestmark = pytest.mark.gpu
 
@@ -88,6 +88,27 @@ def test_a_balanced_router_has_no_gradient(B):
     choices = (torch.arange(96, device="cuda")[:, None] + torch.arange(3, device="cuda")) % 12
     got = B.balance_loss(x, choices, weight=0.5)
     assert not bool(got.grad.any()) and abs(float(got.loss) - 0.5) < 1e-6 and bool((got.counts == 24).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("experts", [7, 64, 512])
+def test_choices_forced_by_the_largest_value(B, dtype, experts):
+    """Logits of the type's largest value: the probabilities are 1, 1/2 and 0.  Tolerance: a share's rounding, the row's sums, the reciprocal (2 units), three products:
+    below 16 EPS of twice the largest share apart from the mean."""
+    x = torch.zeros(40, experts, device="cuda", dtype=dtype)
+    x[:, 3] = torch.finfo(dtype).max
+    x[20:, 5] = torch.finfo(dtype).max
+    choices = torch.full((40, 1), 3, device="cuda")
+    choices[30:] = 5
+    got = B.balance_loss(x, choices, weight=1.0)
+    p = torch.softmax(x.double(), -1)
+    share = torch.bincount(choices.flatten(), minlength=experts).double() / 40
+    apart = share - 1.0 / experts
+    grad = experts / 40 * p * (apart - (p * apart).sum(-1, keepdim=True))
+    assert_within(got.grad, grad, experts / 40 * p * 32 * EPS * apart.abs().max() + rounding(grad, dtype), "gradient")
+    assert_within(got.probs, p.mean(0), 48 * EPS * p.mean(0), "probs")            # (40 additions at most, and the probabilities' own four)
+    loss = experts * (share * p.mean(0)).sum()
+    assert_within(got.loss, loss, 50 * EPS * loss, "loss")
 
 
 def test_gradient_against_differences(B):
