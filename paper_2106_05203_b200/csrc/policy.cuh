@@ -126,23 +126,28 @@ __device__ __forceinline__ void policy_tokens(const float (&lp)[N], const float 
         float farthest = 0.f;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const bool in = ALL || (w >> (8 * e) & 255u) != 0;
             const float delta = ref[e] - lp[e];
-            const bool close = fabsf(delta) <= 1.f;
             farthest = delta != delta ? INFINITY : fmaxf(farthest, fabsf(delta));
-            const float k = close ? exp_minus_line(delta) : 0.f;
-            kl += in ? k : 0.f;
-            g[e] -= close ? s.kl_weight * (k + delta) : 0.f;
         }
-        // far from 0 the slope exp(delta) - 1 comes first: taken from the difference, -1 would be lost where a reference all but rules a token out
-        if (!(farthest <= 1.f)) {
+        if (farthest <= 1.f) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const bool in = ALL || (w >> (8 * e) & 255u) != 0;
+                const float delta = ref[e] - lp[e], k = exp_minus_line(delta);
+                kl += in ? k : 0.f;
+                g[e] -= s.kl_weight * (k + delta);
+            }
+        } else {
+            // far from 0 the slope exp(delta) - 1 comes first: taken from the difference, -1 would be lost where a reference all but rules a token out
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 const bool in = ALL || (w >> (8 * e) & 255u) != 0;
                 const float delta = ref[e] - lp[e];
-                if (fabsf(delta) <= 1.f) continue;
-                const float slope = expf(delta) - 1.f;
-                kl += in ? slope - delta : 0.f;
+                const bool close = fabsf(delta) <= 1.f;
+                float k, slope;
+                if (close) { k = exp_minus_line(delta); slope = k + delta; }
+                else { slope = expf(delta) - 1.f; k = slope - delta; }
+                kl += in ? k : 0.f;
                 g[e] -= s.kl_weight * slope;
             }
         }
