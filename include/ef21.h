@@ -367,7 +367,8 @@ ef21_status ef21_token_logprobs(const void* logits_dev, int32_t dtype, int64_t b
                                 float* lse_out_dev, void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
 /* The logits' gradient, given that of the log-probabilities (grad_dev[batch][length]) and the forward pass's lse_dev:
  * out_j = scale grad (1[j = target] - exp(scale x_j - lse)), in the logits' type.  out may be the logits themselves (same strides), or must not
- * overlap them.  Rows that are ignored, whose grad is 0, or whose lse is -inf get zeros and are not read. */
+ * overlap them.  Rows that are ignored, whose grad is 0, or whose lse is -inf get zeros and are not read.  lse is fp32: probabilities are off by |lse| 2^-24
+ * relative, so a row of nothing but lowest values (lse holds no log of their number any more) is to be ignored or to have a grad of 0. */
 ef21_status ef21_token_logprobs_grad(const void* logits_dev, int32_t dtype, int64_t batch, int64_t length, int64_t vocab,
                                      int64_t batch_stride, int64_t row_stride, const void* targets_dev, int32_t index_type,
                                      int64_t targets_batch_stride, const float* lse_dev, const float* grad_dev, float scale,

@@ -8,7 +8,8 @@
 // launch add up the longer runs ED_CHUNK sorted positions at a time; a last launch joins these sums, in order.
 //
 // Lookup of 16,384 x 4,096 bf16: 32.5 us, 5.9 TB/s.  Gradient of 65,536 tokens (the most frequent 6,000 times) into 50,257 x 2,048 fp32: 167 us; the sums 130 (700 MB), the sort
-// in front of them 24, the join behind them 8.  1,000 tokens into 1,024 x 257: 11.8 us.
+// in front of them 24, the join behind them 8.  1,000 tokens into 1,024 x 257 fp32: 10 us; 3,000 into 10,000 x 64 half 18,
+// 8,000 into 500 x 40 bf16 25 (24 and 28 with two positions in flight, as large tables have).
 //
 // Sorting: up to ED_RANK_TOKENS tokens by counting, for every token, those in front of it -- one launch; more by a radix sort, digits of up to nine bits, three launches
 // each.  (All passes in the shared memory of one cluster were measured, too: 4 us faster at 9,000 tokens, as fast at 30,000, 10 us slower at 65,000.)
@@ -104,7 +105,8 @@ __device__ __forceinline__ int token_key(const void* tokens, int wide, i64 i, i6
     return v >= 0 && v < vocab && v != padding ? (int)v : (int)vocab;
 }
 
-// Few tokens: the place of each is the number of smaller ones plus that of equal ones before it.  A warp takes one token at a time.
+// Few tokens: the place of each is the number of smaller ones plus that of equal ones before it -- of those not larger in front of it and of smaller ones behind it.  A
+// warp takes one token at a time.
 __global__ void __launch_bounds__(ED_RANK_THREADS) embedding_rank_kernel(const void* tokens, int wide, int count, i64 vocab, i64 padding, int2* sorted, int2* runs) {
     pdl_wait(tokens, sorted, runs);
     pdl_trigger();
@@ -122,21 +124,21 @@ __global__ void __launch_bounds__(ED_RANK_THREADS) embedding_rank_kernel(const v
     }
     __syncthreads();
     for (int i = blockIdx.x * (ED_RANK_THREADS / 32) + (threadIdx.x >> 5); i < count; i += gridDim.x * (ED_RANK_THREADS / 32)) {
-        const int key = keys[i];
-        int less = 0, before = 0, equal = 0;
+        const int key = keys[i], own = i / 4;
+        int less = 0, up_to = 0, place = 0;                               // smaller ones, and those not larger
 #pragma unroll 4
-        for (int j = lane * 4; j < padded; j += 128) {
-            const int4 v = *reinterpret_cast<const int4*>(keys + j);
-            less += (v.x < key) + (v.y < key) + (v.z < key) + (v.w < key);
-            equal += (v.x == key) + (v.y == key) + (v.z == key) + (v.w == key);
-            before += (v.x == key && j < i) + (v.y == key && j + 1 < i) + (v.z == key && j + 2 < i) + (v.w == key && j + 3 < i);
+        for (int j = lane; j < padded / 4; j += 32) {
+            const int4 v = *reinterpret_cast<const int4*>(keys + j * 4);
+            const int low = (v.x < key) + (v.y < key) + (v.z < key) + (v.w < key), up = (v.x <= key) + (v.y <= key) + (v.z <= key) + (v.w <= key);
+            less += low; up_to += up; place += j < own ? up : low;
         }
+        if (lane < i - own * 4) place += keys[own * 4 + lane] == key;     // (in front of it among its own four)
+        place = __reduce_add_sync(0xffffffffu, place);
         less = __reduce_add_sync(0xffffffffu, less);
-        equal = __reduce_add_sync(0xffffffffu, equal);
-        before = __reduce_add_sync(0xffffffffu, before);
+        up_to = __reduce_add_sync(0xffffffffu, up_to);
         if (lane == 0) {
-            sorted[less + before] = make_int2(key, i);
-            if (before == 0 && key < vocab) runs[key] = make_int2(less, less + equal);
+            sorted[place] = make_int2(key, i);
+            if (place == less && key < vocab) runs[key] = make_int2(less, up_to);
         }
     }
 }
@@ -306,11 +308,11 @@ struct Columns {
     __device__ __forceinline__ bool in(int k) const { return at(k) < dim; }
 };
 
-// Sums over sorted positions [begin, end), in order.  16-bit vectors: two at a time, what is left over alone (registers; whatever else was tried costs the large table 3 %).
-// Others: four or eight at a time, the next ones' places looked up meanwhile -- small tables wait for the longest run.
-template <typename T, int VEC, int VECS>
+// Sums over sorted positions [begin, end), in order.  MANY teams and 16-bit vectors: two at a time, what is left over alone (registers; whatever else was tried costs the
+// large table 3 %).  Others: four or eight at a time, the next ones' places looked up meanwhile -- small tables wait for the longest run.
+template <bool MANY, typename T, int VEC, int VECS>
 __device__ __forceinline__ void add_run(const T* grad, i64 stride, const int2* sorted, int begin, int end, const Columns<VEC, VECS>& c, float (&sum)[VECS][VEC]) {
-    if constexpr (VEC == 8) {
+    if constexpr (VEC == 8 && MANY) {
         auto two_or_one = [&](int i, auto n) {
             constexpr int N = decltype(n)::value;
             const T* g[N];
@@ -336,7 +338,7 @@ __device__ __forceinline__ void add_run(const T* grad, i64 stride, const int2* s
         if (i < end) two_or_one(i, std::integral_constant<int, 1>{});
         return;
     }
-    constexpr int N = VEC == 1 && VECS == ED_SINGLES ? 8 : 4;
+    constexpr int N = MANY ? 4 : 8;
     int at[N];
 #pragma unroll
     for (int p = 0; p < N; ++p) at[p] = begin + p < end ? sorted[begin + p].y : 0;
@@ -442,7 +444,7 @@ __global__ void __launch_bounds__(ED_THREADS) embedding_fill_kernel(O* out, i64 
 // MANY: there are more teams than the device holds; fewer of them, with more columns and, one after the other, ED_ROWS rows each, take less of everything.
 // Otherwise the launch takes as long as its longest run.
 template <typename T, typename O, bool VECTORS, bool MANY>
-__global__ void __launch_bounds__(ED_SUM_THREADS, 12) embedding_sums_kernel(const T* grad, const int2* sorted, const int2* runs, float* partial, O* out, TableShape s) {
+__global__ void __launch_bounds__(ED_SUM_THREADS, MANY || !VECTORS ? 12 : 8) embedding_sums_kernel(const T* grad, const int2* sorted, const int2* runs, float* partial, O* out, TableShape s) {
     pdl_wait(grad, sorted, runs, partial, out);
     pdl_trigger();
     constexpr int VEC = VECTORS ? Elem<T>::VEC : 1, VECS = VECTORS ? ED_VECS : MANY ? ED_MANY_SINGLES : ED_SINGLES, ROWS = MANY ? ED_ROWS : 1;
@@ -464,7 +466,7 @@ __global__ void __launch_bounds__(ED_SUM_THREADS, 12) embedding_sums_kernel(cons
             const int2 run = runs[key];
             if (run.y - run.x <= ED_CHUNK) continue;
             float sum[VECS][VEC] = {};
-            add_run<T, VEC, VECS>(grad, s.stride, sorted, max(run.x, (int)c0), min(run.y, (int)c1), c, sum);
+            add_run<MANY, T, VEC, VECS>(grad, s.stride, sorted, max(run.x, (int)c0), min(run.y, (int)c1), c, sum);
             float* p = partial + (at * 2 + slot) * s.dim;
 #pragma unroll
             for (int k = 0; k < VECS; ++k) if (c.in(k)) put_floats<VEC>(p + c.at(k), sum[k]);
@@ -484,7 +486,7 @@ __global__ void __launch_bounds__(ED_SUM_THREADS, 12) embedding_sums_kernel(cons
         float sum[VECS][VEC];
         one.fetch(grad + (i64)head[0].y * s.stride, c, true);
         one.take(sum);
-        if (run[0].y - run[0].x > 1) add_run<T, VEC, VECS>(grad, s.stride, sorted, run[0].x + 1, run[0].y, c, sum);
+        if (run[0].y - run[0].x > 1) add_run<MANY, T, VEC, VECS>(grad, s.stride, sorted, run[0].x + 1, run[0].y, c, sum);
         put_row<O, VEC, VECS>(out + (i64)head[0].x * s.out_stride, c, sum, s);
         return;
     }
@@ -507,7 +509,7 @@ __global__ void __launch_bounds__(ED_SUM_THREADS, 12) embedding_sums_kernel(cons
             next.fetch(grad + (i64)head[(r + 1) % ROWS].y * s.stride, c, m > 0 && m <= ED_CHUNK);
         }
         if (first + r >= s.vocab || n > ED_CHUNK || (n == 0 && s.accumulate)) continue;
-        if (n > 1) add_run<T, VEC, VECS>(grad, s.stride, sorted, run[r].x + 1, run[r].y, c, sum);
+        if (n > 1) add_run<MANY, T, VEC, VECS>(grad, s.stride, sorted, run[r].x + 1, run[r].y, c, sum);
         put_row<O, VEC, VECS>(out + (first + r) * s.out_stride, c, sum, s);
     }
 }
