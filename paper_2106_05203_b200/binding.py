@@ -675,6 +675,8 @@ def token_logprobs_grad(logits: torch.Tensor, targets: torch.Tensor, lse: torch.
         _rows_apart(out, "out")
         if not (out.data_ptr() == logits.data_ptr() and out.stride() == logits.stride()) and _overlap(out, logits):
             raise ValueError("out must be the logits, or apart from them")
+        if any(_overlap(out, t) for t in (targets, lse, grad)):
+            raise ValueError("out must be apart from targets, lse and grad")
     device = _same_device(logits, targets, lse, grad, out)
     there = _elsewhere(device, stream)
     if there is not None:
@@ -861,8 +863,8 @@ def embedding_grad(grad: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: 
     if out is not None:
         out_stride = _matrix(out, "out", (vocab, dim))
         _rows_apart(out, "out")
-        if _overlap(out, grad):
-            raise ValueError("out must be apart from grad")
+        if _overlap(out, grad) or _overlap(out, tokens):
+            raise ValueError("out must be apart from grad and tokens")
     device = _same_device(grad, tokens, out)
     there = _elsewhere(device, stream)
     if there is not None:

@@ -145,3 +145,14 @@ def test_the_binding_refuses(error, call):
 def test_there_is_no_cpu_path(call):
     with pytest.raises(TypeError, match="CUDA"):
         call()
+
+
+def test_outputs_on_what_is_still_read():
+    """An output that lies on the other inputs of its call: rows would be looked up in what has been overwritten."""
+    lse, grad = torch.zeros(4), torch.zeros(4)
+    for shared in (lse, grad):
+        with pytest.raises(ValueError, match="apart"):
+            B.token_logprobs_grad(torch.zeros(4, 1), torch.zeros(4, dtype=torch.int64), lse, grad, out=shared.view(4, 1))
+    store = torch.zeros(16)
+    with pytest.raises(ValueError, match="apart"):
+        B.embedding_grad(torch.zeros(4, 3), store[:4].view(torch.int32), 5, out=store[:15].view(5, 3))
