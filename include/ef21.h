@@ -355,6 +355,9 @@ enum {
     EF21_REDUCE_TOKENS = 0,   /* every token that counts weighs the same */
     EF21_REDUCE_SEQUENCES = 1 /* every row with such tokens weighs the same, its tokens alike */
 };
+/* What the workspace queries below answer where the call keeps nothing in its workspace: the address has to be there and aligned, nothing is read
+ * or written.  A call that keeps something, be it 16 bytes, asks for more.  (0: no such call.) */
+enum { EF21_NO_WORKSPACE = 256 };
 
 /* Log-probabilities of given tokens: lse = log sum_j exp(scale x_j), logp = scale x_target - lse, for `batch` times `length` rows of
  * `vocab` logits; row (b, t) starts at b batch_stride + t row_stride, its target is targets[b targets_batch_stride + t].

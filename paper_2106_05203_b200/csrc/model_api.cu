@@ -48,6 +48,8 @@ struct Sections {
         return p;
     }
 };
+// What a size query answers for `used` bytes: a call that keeps something asks for more than EF21_NO_WORKSPACE, however little it is.
+size_t workspace_size(size_t used) { return used == 0 ? (size_t)EF21_NO_WORKSPACE : used > EF21_NO_WORKSPACE ? used : EF21_NO_WORKSPACE + ALIGN; }
 bool workspace_fits(const void* p, size_t have, size_t need) { return p != nullptr && have >= need && aligned(p, ALIGN); }
 
 // ---- token log-probabilities --------------------------------------------------------------------------------------------------------------
@@ -170,7 +172,7 @@ extern "C" {
 size_t ef21_token_logprobs_workspace_bytes(int32_t dtype, int64_t batch, int64_t length, int64_t vocab) {
     if (!valid_logits(dtype, batch, length, vocab, EF21_INDEX_I64, 1.f)) return 0;
     const i64 units = logprob_units(dtype, batch * length, vocab);
-    return units == 0 ? ALIGN : align_up(sizeof(float2) * (size_t)(batch * length) * (size_t)units);
+    return workspace_size(align_up(sizeof(float2) * (size_t)(batch * length) * (size_t)units));
 }
 
 ef21_status ef21_token_logprobs(const void* logits_dev, int32_t dtype, int64_t batch, int64_t length, int64_t vocab, int64_t batch_stride, int64_t row_stride,
@@ -231,7 +233,7 @@ ef21_status ef21_token_logprobs_grad(const void* logits_dev, int32_t dtype, int6
 size_t ef21_preference_loss_workspace_bytes(int64_t pairs, int64_t length) {
     if (pairs < 1 || pairs > MOST / 16 || length < 0 || length > MOST) return 0;
     const PreferencePlan p = preference_plan(pairs, length);
-    return p.one ? ALIGN : align_up(sizeof(double) * (size_t)p.losses);
+    return workspace_size(p.one ? 0 : align_up(sizeof(double) * (size_t)p.losses));
 }
 
 ef21_status ef21_preference_loss(const void* logps_dev, const void* ref_dev, const uint8_t* mask_dev, int32_t dtype, int64_t pairs, int64_t length,
@@ -267,7 +269,7 @@ ef21_status ef21_preference_loss(const void* logps_dev, const void* ref_dev, con
 
 size_t ef21_policy_loss_workspace_bytes(int64_t rows, int64_t length) {
     PolicyWork w;
-    return valid_rows(rows, length) ? policy_layout(nullptr, rows, w) : 0;
+    return valid_rows(rows, length) ? workspace_size(policy_layout(nullptr, rows, w)) : 0;
 }
 
 ef21_status ef21_policy_loss(const void* logps_dev, const void* old_dev, const void* ref_dev, const void* advantages_dev, const uint8_t* mask_dev, int32_t dtype,
@@ -316,7 +318,7 @@ ef21_status ef21_policy_loss(const void* logps_dev, const void* old_dev, const v
 
 size_t ef21_balance_loss_workspace_bytes(int64_t rows, int64_t experts) {
     BalanceBuffers w;
-    return rows < 0 || rows > MOST || experts < 1 || experts > BL_MAX_EXPERTS ? 0 : balance_layout(nullptr, rows, experts, w);
+    return rows < 0 || rows > MOST || experts < 1 || experts > BL_MAX_EXPERTS ? 0 : workspace_size(balance_layout(nullptr, rows, experts, w));
 }
 
 ef21_status ef21_balance_loss(const void* logits_dev, int32_t dtype, int64_t rows, int64_t experts, int64_t logits_stride, const void* choices_dev, int32_t index_type, int64_t chosen,
@@ -386,7 +388,7 @@ ef21_status ef21_embedding(const void* weight_dev, int32_t dtype, int64_t vocab,
 
 size_t ef21_embedding_grad_workspace_bytes(int64_t count, int64_t vocab, int64_t dim) {
     EmbeddingWork w;
-    return valid_table(count, vocab, dim) ? embedding_layout(nullptr, count, vocab, dim, w) : 0;
+    return valid_table(count, vocab, dim) ? workspace_size(embedding_layout(nullptr, count, vocab, dim, w)) : 0;
 }
 
 ef21_status ef21_embedding_grad(const void* grad_dev, int32_t dtype, int64_t count, int64_t dim, int64_t grad_stride, const void* tokens_dev, int32_t index_type, int64_t vocab,

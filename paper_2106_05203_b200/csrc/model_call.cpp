@@ -54,9 +54,9 @@ struct Call {
         return at::empty(sizes, at::TensorOptions().device(at::Device(at::kCUDA, (c10::DeviceIndex)device)).dtype(type));
     }
     void* stream() const { return c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream(); }
-    // `bytes` of workspace; up to ALIGN they are looked at, not used: any aligned address does
+    // `bytes` of workspace; EF21_NO_WORKSPACE of them are looked at, not used: any aligned address does
     void* workspace(size_t bytes, const at::Tensor& other, at::Tensor& keep) const {
-        if (bytes <= ALIGN && reinterpret_cast<uintptr_t>(other.data_ptr()) % ALIGN == 0) return other.data_ptr();
+        if (bytes == EF21_NO_WORKSPACE && reinterpret_cast<uintptr_t>(other.data_ptr()) % ALIGN == 0) return other.data_ptr();
         keep = make({(int64_t)(bytes + ALIGN)}, at::kByte);
         return reinterpret_cast<void*>((reinterpret_cast<uintptr_t>(keep.data_ptr()) + ALIGN - 1) / ALIGN * ALIGN);
     }
