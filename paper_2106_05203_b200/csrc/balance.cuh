@@ -21,6 +21,7 @@ constexpr int BL_MAX_EXPERTS = 1024;
 constexpr int BL_MAX_BLOCKS = 148 * 3;         // (registers for three blocks an SM)
 constexpr int BL_FINISH_COLUMNS = 8, BL_FINISH_GROUPS = 128;
 constexpr unsigned BL_CLUSTER = 8;
+constexpr float BL_FUSED = 1e6f;               // logits up to here: the exponent by one operation
 constexpr i64 BL_ONE_CHOICES = 16384, BL_ONE_LOGITS = 32768;      // up to here: one cluster
 
 struct BalanceShape {
@@ -173,7 +174,10 @@ __global__ void __launch_bounds__(BL_THREADS, PER * Elem<T>::VEC <= 16 ? 3 : 1) 
         for (int r = 0; r < ROWS; ++r) {
             float base = top[r] == -INFINITY ? 0.f : top[r];                 // (a row of -inf only, or left out: all 0)
             const Two exponent = two(LOG2E);
-            if (fabsf(base) > 1e38f) {                                       // (a mask of the type's lowest value, a choice forced by its largest: it times log2 e would overflow)
+            // The exponent is one fused operation about base log2 e, whose rounding all of the row have in common: it cancels in p as long as it is small (0.06 in base 2
+            // at the border).  Beyond -- a mask of a large value that leaves nothing, a choice forced by one -- it would leave the range of 2^x, and the maximum is
+            // subtracted first.
+            if (fabsf(base) > BL_FUSED) {
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) f[r][i] = add2(f[r][i], two(-base));
                 base = 0.f;
