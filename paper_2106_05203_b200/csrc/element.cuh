@@ -132,10 +132,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
-// e^x to a few units in the last place: what the product with log2 e loses is put back to first order.  (Below 2^-126: 0.)
+// e^x to a few units in the last place: what the product with log2 e loses is put back to first order.  (Below 2^-126: 0.)  Where 2^t is 0, infinite or NaN there is nothing to put
+// back to: infinity less a little is NaN.
 __device__ __forceinline__ float exp_fast(float x) {
     const float t = x * LOG2E, y = exp2_fast(t), lost = fmaf(x, LOG2E, -t);
-    return fabsf(lost) <= 1.f ? fmaf(y, lost * LN2, y) : y;              // (infinite t: nothing to put back)
+    return fabsf(t) < 128.f ? fmaf(y, lost * LN2, y) : y;
 }
 
 // Two fp32 values, and one instruction for both.
