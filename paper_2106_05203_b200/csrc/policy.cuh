@@ -123,6 +123,7 @@ __device__ __forceinline__ void policy_tokens(const float (&lp)[N], const float 
         g[e] = cut[e] ? 0.f : -gain;
     }
     if (has_ref) {
+        const bool in_loss = s.kl_weight != 0.f;                          // (a term that is only told has no slope, be it infinite)
         float farthest = 0.f;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
@@ -135,7 +136,7 @@ __device__ __forceinline__ void policy_tokens(const float (&lp)[N], const float 
                 const bool in = ALL || (w >> (8 * e) & 255u) != 0;
                 const float delta = ref[e] - lp[e], k = exp_minus_line(delta);
                 kl += in ? k : 0.f;
-                g[e] -= s.kl_weight * (k + delta);
+                if (in_loss) g[e] -= s.kl_weight * (k + delta);
             }
         } else {
             // far from 0 the slope exp(delta) - 1 comes first: taken from the difference, -1 would be lost where a reference all but rules a token out
@@ -148,7 +149,7 @@ __device__ __forceinline__ void policy_tokens(const float (&lp)[N], const float 
                 if (close) { k = exp_minus_line(delta); slope = k + delta; }
                 else { slope = expf(delta) - 1.f; k = slope - delta; }
                 kl += in ? k : 0.f;
-                g[e] -= s.kl_weight * slope;
+                if (in_loss) g[e] -= s.kl_weight * slope;
             }
         }
     }
