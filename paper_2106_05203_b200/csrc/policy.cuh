@@ -159,6 +159,34 @@ __device__ __forceinline__ void policy_tokens(const float (&lp)[N], const float 
     }
 }
 
+constexpr float PO_MOST = 3.402823466e38f;   // the largest finite fp32
+
+// One token whose terms are beyond fp32 before their weight: what is infinite (or NaN) in 32 bits is formed in 64, weighted there, rounded once.  pg, kl and clip are those of
+// policy_tokens; the result is the weighted gradient, the weighted terms are added to the sums.
+__device__ __forceinline__ float far_token(float lp, float old, float ref, bool has_ref, float A, float pg, float kl, float clip, float weighs, const PolicyShape& s, PolicySums& sums) {
+    double P = (double)pg, slope = 0.0;
+    if (fabsf(pg) <= PO_MOST || clip != 0.f) {
+        sums.pg += (double)(weighs * pg);                                 // (as any token's)
+    } else {
+        P = -exp((double)lp - (double)old) * (double)A;
+        sums.pg += (double)weighs * P;
+    }
+    if (has_ref) {
+        const double delta = (double)ref - (double)lp;
+        if (fabsf(kl) <= PO_MOST) {
+            slope = (double)kl + delta;
+            sums.kl += (double)(weighs * kl);
+        } else {
+            slope = exp(delta) - 1.0;
+            sums.kl += (double)weighs * (slope - delta);
+        }
+    }
+    sums.clipped += (double)(weighs * clip);
+    double g = clip != 0.f ? 0.0 : P;
+    if (s.kl_weight != 0.f) g -= (double)s.kl_weight * slope;
+    return (float)((double)weighs * g);
+}
+
 // FLAT: all arrays are contiguous, a vector of VEC tokens may run over the end of a row.  Otherwise token by token, any strides.
 template <typename T, bool FLAT>
 __global__ void __launch_bounds__(PO_THREADS) policy_kernel(const T* logps, const T* old, const T* ref, const T* adv, const unsigned char* mask, const int* tokens, const i64* counted,
@@ -238,6 +266,10 @@ __global__ void __launch_bounds__(PO_THREADS) policy_kernel(const T* logps, cons
         const float f[1] = {ref ? Elem<T>::get(ref[row * s.ref_stride + t]) : 0.f};
         float v[1];
         policy_tokens<1, true, unsigned>(x, o, f, ref != nullptr, a, 1u, s, v, pg, kl, clip);
+        if (!(fabsf(pg) + fabsf(kl) <= PO_MOST)) {
+            *g = Elem<T>::put(far_token(x[0], o[0], f[0], ref != nullptr, A, pg, kl, clip, weighs, s, sums));
+            return;
+        }
         *g = Elem<T>::put(weighs * v[0]);
         sums.pg += (double)(weighs * pg); sums.kl += (double)(weighs * kl); sums.clipped += (double)(weighs * clip);
     };
@@ -268,18 +300,27 @@ __global__ void __launch_bounds__(PO_THREADS) policy_kernel(const T* logps, cons
                     for (int e = 0; e < VEC; ++e) A[e] = a;
                 }
                 float pg = 0.f, kl = 0.f, clip = 0.f;
-                if (t + VEC <= s.length) {
+                const bool in_row = t + VEC <= s.length;               // else it runs over the end of one
+                if (in_row) {
                     // (a word of ones: all; other bytes may stand for true, they are looked at one by one)
                     if (!mask || w == (Word)0x0101010101010101ull) policy_tokens<VEC, true, Word>(x, o, f, ref != nullptr, A, w, s, g, pg, kl, clip);
                     else policy_tokens<VEC, false, Word>(x, o, f, ref != nullptr, A, w, s, g, pg, kl, clip);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) g[e] *= weighs;
-                } else {                                               // it runs over the end of a row
+                }
+                if (!in_row || !(fabsf(pg) + fabsf(kl) <= PO_MOST)) {  // (or a term, or the sum of some, is beyond 32 bits)
+                    const PolicySums before = sums;
 #pragma unroll 1
                     for (int e = 0; e < VEC; ++e) token(i + e);
+                    if (in_row) {                                      // a term that is not beyond them is added up as any other vector's: the other one leaves no trace in it
+                        if (fabsf(pg) <= PO_MOST) sums.pg = before.pg + (double)(weighs * pg);
+                        if (fabsf(kl) <= PO_MOST) sums.kl = before.kl + (double)(weighs * kl);
+                        sums.clipped = before.clipped + (double)(weighs * clip);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) g[e] *= weighs;
+                    store_vec(grad + i, Elem<T>::pack(g));
+                    sums.pg += (double)(weighs * pg); sums.kl += (double)(weighs * kl); sums.clipped += (double)(weighs * clip);
                 }
-                if (t + VEC <= s.length) store_vec(grad + i, Elem<T>::pack(g));
-                sums.pg += (double)(weighs * pg); sums.kl += (double)(weighs * kl); sums.clipped += (double)(weighs * clip);
             }
             row += skip_rows; t += skip;
             if (t >= s.length) { t -= s.length; ++row; }
