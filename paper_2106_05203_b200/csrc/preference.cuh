@@ -64,6 +64,12 @@ __device__ __forceinline__ RowPart row_part(i64 length, i64 head, unsigned part,
     return r;
 }
 
+// A token's log ratio: rounded once in 32 bits, and in 64 where it is beyond them (the lowest value on one side, the largest on the other).
+__device__ __forceinline__ double log_ratio(float logp, float ref) {
+    const float d = logp - ref;
+    return fabsf(d) <= 3.4028234e38f ? (double)d : (double)logp - (double)ref;
+}
+
 template <typename T, bool VECTORS, int TEAM>
 __global__ void __launch_bounds__(PF_THREADS) preference_kernel(const T* logps, const T* ref, const unsigned char* mask, float* rewards, T* grad, double* partial, float* loss_out,
                                                                 PreferenceShape s) {
@@ -128,7 +134,7 @@ __global__ void __launch_bounds__(PF_THREADS) preference_kernel(const T* logps, 
         } else {
 #pragma unroll
             for (int side = 0; side < 2; ++side)
-                if (w[side]) sum[side] += (double)(Elem<T>::get(a[side][r[side].body + v]) - (b[side] ? Elem<T>::get(b[side][r[side].body + v]) : 0.f));
+                if (w[side]) sum[side] += log_ratio(Elem<T>::get(a[side][r[side].body + v]), b[side] ? Elem<T>::get(b[side][r[side].body + v]) : 0.f);
         }
     }
     auto ends = [&](int side, auto one) {                          // the elements around the vectors: fewer than a team
@@ -139,7 +145,7 @@ __global__ void __launch_bounds__(PF_THREADS) preference_kernel(const T* logps, 
     if (VECTORS) {
 #pragma unroll
         for (int side = 0; side < 2; ++side)
-            ends(side, [&](i64 j) { if (!m[side] || m[side][j]) sum[side] += (double)(Elem<T>::get(a[side][j]) - (b[side] ? Elem<T>::get(b[side][j]) : 0.f)); });
+            ends(side, [&](i64 j) { if (!m[side] || m[side][j]) sum[side] += log_ratio(Elem<T>::get(a[side][j]), b[side] ? Elem<T>::get(b[side][j]) : 0.f); });
     }
     if (TEAM == 32) {
         sum[0] = warp_sum(sum[0]); sum[1] = warp_sum(sum[1]);
