@@ -347,7 +347,7 @@ int64_t ef21_launch_count(const ef21_ctx* ctx);
  * statistics and losses are fp32 or fp64, results are rounded once, in a fixed order: repeated runs agree bit for bit.
  * Strides and offsets are in elements, the last dimension is contiguous; no call holds state, and two calls whose workspaces
  * and outputs are not shared may run at the same time.  Device pointers belong to the current device.  mask arrays hold one byte per entry: not 0 = counts;
- * what a mask leaves out may hold anything, NaN too.
+ * what a mask leaves out may hold anything, NaN too.  A weight (kl_weight, 1 / norm of the policy loss, weight times experts) beyond fp32 is refused as an infinite one is.
  * --------------------------------------------------------------------------------------------- */
 enum { EF21_DTYPE_F32 = 0, EF21_DTYPE_BF16 = 1, EF21_DTYPE_F16 = 2 };
 enum { EF21_INDEX_I32 = 0, EF21_INDEX_I64 = 1 };
@@ -361,7 +361,7 @@ enum { EF21_NO_WORKSPACE = 256 };
 
 /* Log-probabilities of given tokens: lse = log sum_j exp(scale x_j), logp = scale x_target - lse, for `batch` times `length` rows of
  * `vocab` logits; row (b, t) starts at b batch_stride + t row_stride, its target is targets[b targets_batch_stride + t].
- * logps_out and lse_out: [batch][length].  scale > 0 (one over a temperature).  A row whose target is `ignore` is not read: 0 and 0.
+ * logps_out and lse_out: [batch][length].  scale > 0 (one over a temperature; up to 2.3e38).  A row whose target is `ignore` is not read: 0 and 0.
  * A target outside [0, vocab): NaN and NaN.  A row of -inf only: -inf and -inf.  +inf or NaN among the logits: NaN. */
 size_t ef21_token_logprobs_workspace_bytes(int32_t dtype, int64_t batch, int64_t length, int64_t vocab);
 ef21_status ef21_token_logprobs(const void* logits_dev, int32_t dtype, int64_t batch, int64_t length, int64_t vocab,

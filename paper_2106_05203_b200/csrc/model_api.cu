@@ -56,7 +56,7 @@ bool workspace_fits(const void* p, size_t have, size_t need) { return p != nullp
 
 bool valid_logits(int32_t dtype, i64 batch, i64 length, i64 vocab, int32_t index, float scale) {
     return valid_dtype(dtype) && valid_index(index) && batch >= 0 && length >= 0 && vocab >= 1 && vocab <= MOST && batch <= MOST && length <= MOST &&
-           batch * length <= MOST && std::isfinite(scale) && scale > 0.f;
+           batch * length <= MOST && std::isfinite(scale * LOG2E) && scale > 0.f;
 }
 
 // Blocks that share a row: one where the rows fill the device, up to eight of at least 2,048 columns each where they do not.
@@ -277,8 +277,8 @@ ef21_status ef21_policy_loss(const void* logps_dev, const void* old_dev, const v
                              int32_t advantages_per_token, double clip_low, double clip_high, double kl_weight, int32_t reduction, double norm,
                              float* terms_out_dev, void* grad_out_dev, void* workspace_dev, size_t workspace_bytes, void* cuda_stream) {
     const size_t need = ef21_policy_loss_workspace_bytes(rows, length);
-    if (need == 0 || !valid_dtype(dtype) || !(clip_low >= 0.0 && clip_low < 1.0) || !(clip_high >= 0.0) || !std::isfinite(clip_high) || !std::isfinite(kl_weight) ||
-        (reduction != EF21_REDUCE_TOKENS && reduction != EF21_REDUCE_SEQUENCES) || !(norm >= 0.0) || !std::isfinite(norm) || (!ref_dev && kl_weight != 0.0))
+    if (need == 0 || !valid_dtype(dtype) || !(clip_low >= 0.0 && clip_low < 1.0) || !(clip_high >= 0.0) || !std::isfinite(clip_high) || !std::isfinite((float)kl_weight) ||
+        (reduction != EF21_REDUCE_TOKENS && reduction != EF21_REDUCE_SEQUENCES) || !(norm >= 0.0) || !std::isfinite(norm) || (norm > 0.0 && !std::isfinite((float)(1.0 / norm))) || (!ref_dev && kl_weight != 0.0))
         return EF21_ERR_INVALID_ARG;
     if (!terms_out_dev || (rows * length > 0 && (!logps_dev || !old_dev || !advantages_dev || !grad_out_dev))) return EF21_ERR_INVALID_ARG;
     const size_t e = bytes_of(dtype);
@@ -325,7 +325,7 @@ ef21_status ef21_balance_loss(const void* logits_dev, int32_t dtype, int64_t row
                               int64_t choices_stride, const uint8_t* mask_dev, double weight, float* loss_out_dev, int32_t* counts_out_dev, float* probs_out_dev, void* grad_out_dev,
                               void* workspace_dev, size_t workspace_bytes, void* cuda_stream) {
     const size_t need = ef21_balance_loss_workspace_bytes(rows, experts);
-    if (need == 0 || !valid_dtype(dtype) || !valid_index(index_type) || chosen < 1 || chosen > experts || rows * chosen > MOST || !std::isfinite(weight)) return EF21_ERR_INVALID_ARG;
+    if (need == 0 || !valid_dtype(dtype) || !valid_index(index_type) || chosen < 1 || chosen > experts || rows * chosen > MOST || !std::isfinite((float)(weight * (double)experts))) return EF21_ERR_INVALID_ARG;
     if (!loss_out_dev || !counts_out_dev || !probs_out_dev || (rows > 0 && (!logits_dev || !choices_dev || !grad_out_dev))) return EF21_ERR_INVALID_ARG;
     if (!aligned(logits_dev, bytes_of(dtype)) || !aligned(grad_out_dev, bytes_of(dtype))) return EF21_ERR_INVALID_ARG;
     if (!workspace_fits(workspace_dev, workspace_bytes, need)) return EF21_ERR_WORKSPACE;
