@@ -346,7 +346,8 @@ int64_t ef21_launch_count(const ef21_ctx* ctx);
  * loss of a router that is added to either -- each with its gradient.  Tensors may be fp32, bfloat16 or half; sums, softmax
  * statistics and losses are fp32 or fp64, results are rounded once, in a fixed order: repeated runs agree bit for bit.
  * Strides and offsets are in elements, the last dimension is contiguous; no call holds state, and two calls whose workspaces
- * and outputs are not shared may run at the same time.  Device pointers belong to the current device.  mask arrays hold one byte per entry: not 0 = counts;
+ * and outputs are not shared may run at the same time.  Device pointers belong to the current device and are
+ * multiples of their elements' size.  mask arrays hold one byte per entry: not 0 = counts;
  * what a mask leaves out may hold anything, NaN too.  A weight (kl_weight, 1 / norm of the policy loss, weight times experts) beyond fp32 is refused as an infinite one is.
  * --------------------------------------------------------------------------------------------- */
 enum { EF21_DTYPE_F32 = 0, EF21_DTYPE_BF16 = 1, EF21_DTYPE_F16 = 2 };

@@ -18,6 +18,8 @@ constexpr int SMS = 148;
 cudaStream_t stream_of(void* s) { return reinterpret_cast<cudaStream_t>(s); }
 bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 int bytes_of(int32_t dtype) { return dtype == EF21_DTYPE_F32 ? 4 : 2; }
+bool index_aligned(const void* p, int32_t type) { return aligned(p, type == EF21_INDEX_I64 ? 8 : 4); }
+bool floats_aligned(const void* a, const void* b = nullptr, const void* c = nullptr) { return aligned(a, 4) && aligned(b, 4) && aligned(c, 4); }
 bool valid_dtype(int32_t dtype) { return dtype >= EF21_DTYPE_F32 && dtype <= EF21_DTYPE_F16; }
 bool valid_index(int32_t t) { return t == EF21_INDEX_I32 || t == EF21_INDEX_I64; }
 unsigned grid_of(i64 items, i64 per, i64 most) {
@@ -181,7 +183,9 @@ ef21_status ef21_token_logprobs(const void* logits_dev, int32_t dtype, int64_t b
     if (!valid_logits(dtype, batch, length, vocab, index_type, scale)) return EF21_ERR_INVALID_ARG;
     const i64 rows = batch * length;
     if (rows == 0) return EF21_OK;
-    if (!logits_dev || !targets_dev || !logps_out_dev || !lse_out_dev || !aligned(logits_dev, bytes_of(dtype))) return EF21_ERR_INVALID_ARG;
+    if (!logits_dev || !targets_dev || !logps_out_dev || !lse_out_dev || !aligned(logits_dev, bytes_of(dtype)) || !index_aligned(targets_dev, index_type) ||
+        !floats_aligned(logps_out_dev, lse_out_dev))
+        return EF21_ERR_INVALID_ARG;
     if (!workspace_fits(workspace_dev, workspace_bytes, ef21_token_logprobs_workspace_bytes(dtype, batch, length, vocab))) return EF21_ERR_WORKSPACE;
     const LogprobShape s{length, vocab, batch_stride, row_stride, targets_batch_stride, ignore, index_type, scale};
     return by_dtype(dtype, [&](auto* type) -> ef21_status {
@@ -209,7 +213,8 @@ ef21_status ef21_token_logprobs_grad(const void* logits_dev, int32_t dtype, int6
     if (!valid_logits(dtype, batch, length, vocab, index_type, scale)) return EF21_ERR_INVALID_ARG;
     const i64 rows = batch * length;
     if (rows == 0) return EF21_OK;
-    if (!logits_dev || !targets_dev || !lse_dev || !grad_dev || !out_dev || !aligned(logits_dev, bytes_of(dtype)) || !aligned(out_dev, bytes_of(dtype)))
+    if (!logits_dev || !targets_dev || !lse_dev || !grad_dev || !out_dev || !aligned(logits_dev, bytes_of(dtype)) || !aligned(out_dev, bytes_of(dtype)) ||
+        !index_aligned(targets_dev, index_type) || !floats_aligned(lse_dev, grad_dev))
         return EF21_ERR_INVALID_ARG;
     const LogprobShape s{length, vocab, batch_stride, row_stride, targets_batch_stride, ignore, index_type, scale};
     return by_dtype(dtype, [&](auto* type) -> ef21_status {
@@ -243,7 +248,7 @@ ef21_status ef21_preference_loss(const void* logps_dev, const void* ref_dev, con
     if (need == 0 || !valid_dtype(dtype) || !std::isfinite(beta) || !(smoothing >= 0.0 && smoothing <= 1.0) || !(norm > 0.0) || !std::isfinite(norm)) return EF21_ERR_INVALID_ARG;
     if (!loss_out_dev || !rewards_out_dev || (length > 0 && (!logps_dev || !grad_out_dev))) return EF21_ERR_INVALID_ARG;
     const size_t e = bytes_of(dtype);
-    if (!aligned(logps_dev, e) || !aligned(ref_dev, e) || !aligned(grad_out_dev, e)) return EF21_ERR_INVALID_ARG;
+    if (!aligned(logps_dev, e) || !aligned(ref_dev, e) || !aligned(grad_out_dev, e) || !floats_aligned(loss_out_dev, rewards_out_dev)) return EF21_ERR_INVALID_ARG;
     if (!workspace_fits(workspace_dev, workspace_bytes, need)) return EF21_ERR_WORKSPACE;
     double* partial = static_cast<double*>(workspace_dev);
     const PreferencePlan P = preference_plan(pairs, length);
@@ -282,7 +287,8 @@ ef21_status ef21_policy_loss(const void* logps_dev, const void* old_dev, const v
         return EF21_ERR_INVALID_ARG;
     if (!terms_out_dev || (rows * length > 0 && (!logps_dev || !old_dev || !advantages_dev || !grad_out_dev))) return EF21_ERR_INVALID_ARG;
     const size_t e = bytes_of(dtype);
-    if (!aligned(logps_dev, e) || !aligned(old_dev, e) || !aligned(ref_dev, e) || !aligned(advantages_dev, e) || !aligned(grad_out_dev, e)) return EF21_ERR_INVALID_ARG;
+    if (!aligned(logps_dev, e) || !aligned(old_dev, e) || !aligned(ref_dev, e) || !aligned(advantages_dev, e) || !aligned(grad_out_dev, e) || !floats_aligned(terms_out_dev))
+        return EF21_ERR_INVALID_ARG;
     if (!workspace_fits(workspace_dev, workspace_bytes, need)) return EF21_ERR_WORKSPACE;
     PolicyWork w;
     policy_layout(workspace_dev, rows, w);
@@ -327,7 +333,9 @@ ef21_status ef21_balance_loss(const void* logits_dev, int32_t dtype, int64_t row
     const size_t need = ef21_balance_loss_workspace_bytes(rows, experts);
     if (need == 0 || !valid_dtype(dtype) || !valid_index(index_type) || chosen < 1 || chosen > experts || rows * chosen > MOST || !std::isfinite((float)(weight * (double)experts))) return EF21_ERR_INVALID_ARG;
     if (!loss_out_dev || !counts_out_dev || !probs_out_dev || (rows > 0 && (!logits_dev || !choices_dev || !grad_out_dev))) return EF21_ERR_INVALID_ARG;
-    if (!aligned(logits_dev, bytes_of(dtype)) || !aligned(grad_out_dev, bytes_of(dtype))) return EF21_ERR_INVALID_ARG;
+    if (!aligned(logits_dev, bytes_of(dtype)) || !aligned(grad_out_dev, bytes_of(dtype)) || !index_aligned(choices_dev, index_type) ||
+        !floats_aligned(loss_out_dev, counts_out_dev, probs_out_dev))
+        return EF21_ERR_INVALID_ARG;
     if (!workspace_fits(workspace_dev, workspace_bytes, need)) return EF21_ERR_WORKSPACE;
     BalanceBuffers w;
     balance_layout(workspace_dev, rows, experts, w);
@@ -365,7 +373,7 @@ ef21_status ef21_embedding(const void* weight_dev, int32_t dtype, int64_t vocab,
                            void* out_dev, void* cuda_stream) {
     if (!valid_dtype(dtype) || !valid_index(index_type) || !valid_table(count, vocab, dim) || !std::isfinite(scale)) return EF21_ERR_INVALID_ARG;
     if (count == 0) return EF21_OK;
-    if (!weight_dev || !tokens_dev || !out_dev || !aligned(weight_dev, bytes_of(dtype)) || !aligned(out_dev, bytes_of(dtype))) return EF21_ERR_INVALID_ARG;
+    if (!weight_dev || !tokens_dev || !out_dev || !aligned(weight_dev, bytes_of(dtype)) || !aligned(out_dev, bytes_of(dtype)) || !index_aligned(tokens_dev, index_type)) return EF21_ERR_INVALID_ARG;
     return by_dtype(dtype, [&](auto* type) -> ef21_status {
         typedef typename Pointee<decltype(type)>::type T;
         constexpr int VEC = Elem<T>::VEC;
@@ -396,7 +404,7 @@ ef21_status ef21_embedding_grad(const void* grad_dev, int32_t dtype, int64_t cou
                                 void* cuda_stream) {
     const size_t need = ef21_embedding_grad_workspace_bytes(count, vocab, dim);
     if (need == 0 || !valid_dtype(dtype) || (out_dtype != dtype && out_dtype != EF21_DTYPE_F32) || !valid_index(index_type) || !std::isfinite(scale) || !out_dev ||
-        (count > 0 && (!grad_dev || !tokens_dev)) || !aligned(grad_dev, bytes_of(dtype)) || !aligned(out_dev, bytes_of(out_dtype)))
+        (count > 0 && (!grad_dev || !tokens_dev)) || !aligned(grad_dev, bytes_of(dtype)) || !aligned(out_dev, bytes_of(out_dtype)) || !index_aligned(tokens_dev, index_type))
         return EF21_ERR_INVALID_ARG;
     if (!workspace_fits(workspace_dev, workspace_bytes, need)) return EF21_ERR_WORKSPACE;
     EmbeddingWork w;

@@ -49,3 +49,23 @@ def test_weights_beyond_fp32():
     for weight in (1e38, 1e39, -1e300):
         assert status("ef21_balance_loss", BALANCE, weight=weight) == INVALID          # (times eight experts)
     assert fine("ef21_balance_loss", BALANCE, weight=1e37) and fine("ef21_balance_loss", BALANCE, weight=-1.0)
+
+
+@pytest.mark.parametrize("entry,good,fields,rows", [
+    ("ef21_token_logprobs", LOGPROBS, [("targets", 4), ("logps", 2), ("lse", 2)], {}),
+    ("ef21_token_logprobs_grad", LOGPROBS_GRAD, [("targets", 4), ("lse", 2), ("grad", 2)], {"out": P, "length": 1}),
+    ("ef21_preference_loss", PREFERENCE, [("loss", 2), ("rewards", 2)], {}),
+    ("ef21_policy_loss", POLICY, [("terms", 2)], {}),
+    ("ef21_balance_loss", BALANCE, [("choices", 4), ("loss", 2), ("counts", 2), ("probs", 2)], {}),
+    ("ef21_embedding", EMBEDDING, [("tokens", 4)], {"out": P}),
+    ("ef21_embedding_grad", EMBEDDING_GRAD, [("tokens", 4)], {}),
+])
+def test_addresses_between_two_elements(entry, good, fields, rows):
+    """Indices and fp32 arrays as well as the tensors: a load from there would be a fault of the device.  (Refused before anything else; with a device at hand it is not
+    tried out what became of a call that is not.)"""
+    if torch.cuda.is_available():
+        pytest.skip("entries by themselves, without a device")
+    for field, off in fields:
+        assert status(entry, good, **rows, **{field: P + off}) == INVALID, field
+        if field in ("targets", "choices", "tokens"):
+            assert status(entry, good, **rows, **{field: P + 2, "index": 0}) == INVALID, field
