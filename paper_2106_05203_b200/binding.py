@@ -558,6 +558,9 @@ def _mask(t: Optional[torch.Tensor], shape) -> int:
 
 
 def _same_device(*tensors: Optional[torch.Tensor]) -> torch.device:
+    """The device of a call's tensors, whose memory has to hold their values."""
+    if any(t is not None and t.is_neg() for t in tensors):
+        raise TypeError("a view that takes the negative as it is read (resolve_neg() writes it out)")
     device = tensors[0].device
     if device.type != "cuda":
         raise TypeError("expected CUDA tensors; there is no CPU path")

@@ -42,11 +42,11 @@ struct Released {
 // What a call works on: its device, options of its tensors.
 struct Call {
     int device = -1;
-    // an ordinary tensor on the current device (which is asked for where there is a CUDA tensor: without a GPU there is none)
+    // an ordinary tensor on the current device, whose memory holds its values (the device is asked for where there is a CUDA tensor: without a GPU there is none)
     bool usual(PyObject* o) {
         if (!THPVariable_CheckExact(o)) return false;
         const at::Tensor& t = THPVariable_Unpack(o);
-        if (!t.has_storage() || !t.is_cuda() || t.layout() != at::kStrided) return false;
+        if (!t.has_storage() || !t.is_cuda() || t.layout() != at::kStrided || t.is_neg()) return false;
         if (device < 0) device = c10::cuda::current_device();
         return t.get_device() == device;
     }

@@ -69,3 +69,31 @@ def test_addresses_between_two_elements(entry, good, fields, rows):
         assert status(entry, good, **rows, **{field: P + off}) == INVALID, field
         if field in ("targets", "choices", "tokens"):
             assert status(entry, good, **rows, **{field: P + 2, "index": 0}) == INVALID, field
+
+
+LAZY = [
+    ("token_logprobs", lambda B, t, n: B.token_logprobs(n(2, 8), t.zeros(2, dtype=torch.int64))),
+    ("token_logprobs_grad", lambda B, t, n: B.token_logprobs_grad(t.ones(2, 8), t.zeros(2, dtype=torch.int64), t.ones(2), n(2))),
+    ("preference_loss", lambda B, t, n: B.preference_loss(n(4, 5))),
+    ("preference_loss, reference", lambda B, t, n: B.preference_loss(t.ones(4, 5), n(4, 5))),
+    ("policy_loss", lambda B, t, n: B.policy_loss(t.ones(4, 5), t.ones(4, 5), n(4))),
+    ("balance_loss", lambda B, t, n: B.balance_loss(n(4, 5), t.zeros(4, 1, dtype=torch.int64))),
+    ("embedding", lambda B, t, n: B.embedding(n(4, 5), t.zeros(3, dtype=torch.int64))),
+    ("embedding_grad", lambda B, t, n: B.embedding_grad(n(3, 5), t.zeros(3, dtype=torch.int64), 4)),
+]
+
+
+class On:
+    """torch's constructors on a device."""
+
+    def __init__(self, device):
+        self.zeros = lambda *s, **k: torch.zeros(*s, device=device, **k)
+        self.ones = lambda *s, **k: torch.ones(*s, device=device, **k)
+
+
+@pytest.mark.parametrize("device", ["cpu", pytest.param("cuda", marks=pytest.mark.gpu)])
+@pytest.mark.parametrize("call", [c for _, c in LAZY], ids=[n for n, _ in LAZY])
+def test_negatives_that_are_not_taken_yet(device, call):
+    """What x.conj().imag of a complex x is: the negative is taken when a value is read, the memory holds the opposite."""
+    with pytest.raises(TypeError, match="negative"):
+        call(B, On(device), lambda *s: torch._neg_view(torch.ones(*s, device=device)))
