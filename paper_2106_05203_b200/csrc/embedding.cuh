@@ -30,7 +30,7 @@ constexpr int ED_JOIN_THREADS = 512, ED_SHARES = ED_JOIN_THREADS / 32;
 constexpr int ED_ROWS = 4;                  // rows of the table per team where that leaves enough teams
 constexpr int ED_RANK_TOKENS = 4096;
 constexpr int ED_RANK_THREADS = 256;
-constexpr int RX_THREADS = 1024, RX_ITEMS = 1, RX_TILE = RX_THREADS * RX_ITEMS, RX_MAX_BITS = 9, RX_WARPS = RX_THREADS / 32;
+constexpr int RX_THREADS = 1024, RX_TILE = RX_THREADS, RX_MAX_BITS = 9, RX_WARPS = RX_THREADS / 32;       // an item a thread
 
 // ---- lookup -------------------------------------------------------------------------------------------------------------------------------
 
@@ -156,11 +156,8 @@ __global__ void __launch_bounds__(RX_THREADS) radix_count_kernel(const int2* sou
     const int bins = 1 << bits;
     for (int b = threadIdx.x; b < bins; b += RX_THREADS) here[b] = 0;
     __syncthreads();
-#pragma unroll
-    for (int k = 0; k < RX_ITEMS; ++k) {
-        const i64 i = (i64)blockIdx.x * RX_TILE + k * RX_THREADS + threadIdx.x;
-        if (i < count) atomicAdd(&here[(radix_item(source, tokens, wide, i, vocab, padding).x >> shift) & (bins - 1)], 1);
-    }
+    const i64 i = (i64)blockIdx.x * RX_TILE + threadIdx.x;
+    if (i < count) atomicAdd(&here[(radix_item(source, tokens, wide, i, vocab, padding).x >> shift) & (bins - 1)], 1);
     __syncthreads();
     for (int b = threadIdx.x; b < bins; b += RX_THREADS) counts[(i64)blockIdx.x * bins + b] = here[b];
 }
@@ -188,25 +185,19 @@ __global__ void __launch_bounds__(RX_THREADS) radix_places_kernel(int* counts, i
     }
 }
 
-// The order of a block's items by their digits: item (warp, k, lane) is the rank[k]-th of its digit in its warp.  Leaves the warps' counts.
-template <int ITEMS>
-__device__ __forceinline__ void radix_rank(const int (&digit)[ITEMS], int (&rank)[ITEMS], unsigned short* of_warp, int bits) {
+// How many items of the same digit a warp has in front of a lane's (digit -1: no item).  of_warp[digit] becomes the number of all of them.
+__device__ __forceinline__ int radix_rank(int digit, unsigned short* of_warp, int bits) {
     const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int k = 0; k < ITEMS; ++k) {
-        // lanes with the same digit, bit by bit (a ballot each: the match instruction takes several times as long)
-        unsigned peers = __ballot_sync(0xffffffffu, digit[k] >= 0);
-        for (int b = 0; b < bits; ++b) {
-            const bool one = digit[k] >> b & 1;
-            const unsigned ones = __ballot_sync(0xffffffffu, one);
-            peers &= one ? ones : ~ones;
-        }
-        const int first = __ffs(peers) - 1, ahead = __popc(peers & ((1u << lane) - 1u));
-        int base = 0;
-        if (digit[k] >= 0 && lane == first) { base = of_warp[digit[k]]; of_warp[digit[k]] = (unsigned short)(base + __popc(peers)); }
-        rank[k] = __shfl_sync(0xffffffffu, base, first) + ahead;
-        __syncwarp();
+    // lanes with the same digit, bit by bit (a ballot each: the match instruction takes several times as long)
+    unsigned peers = __ballot_sync(0xffffffffu, digit >= 0);
+    for (int b = 0; b < bits; ++b) {
+        const bool one = digit >> b & 1;
+        const unsigned ones = __ballot_sync(0xffffffffu, one);
+        peers &= one ? ones : ~ones;
     }
+    const int ahead = __popc(peers & ((1u << lane) - 1u));
+    if (digit >= 0 && ahead == 0) of_warp[digit] = (unsigned short)__popc(peers);
+    return ahead;
 }
 
 __global__ void __launch_bounds__(RX_THREADS) radix_move_kernel(const int2* source, const void* tokens, int wide, i64 count, i64 vocab, i64 padding, int shift, int bits,
@@ -222,27 +213,19 @@ __global__ void __launch_bounds__(RX_THREADS) radix_move_kernel(const int2* sour
     const unsigned mine = tid < bins ? (unsigned)totals[tid] : 0u;
     const unsigned before = block_excl_scan(mine, scan, all);
     if (tid < bins) place[tid] = (int)before + counts[(i64)blockIdx.x * bins + tid];
-    // a warp's items are consecutive: (warp, k, lane) is their order
-    int2 item[RX_ITEMS];
-    int digit[RX_ITEMS], rank[RX_ITEMS];
+    const i64 i = (i64)blockIdx.x * RX_TILE + tid;
+    const bool in = i < count;
+    const int2 item = in ? radix_item(source, tokens, wide, i, vocab, padding) : make_int2(0, 0);
+    const int digit = in ? (item.x >> shift) & (bins - 1) : -1;
     __syncwarp();
-#pragma unroll
-    for (int k = 0; k < RX_ITEMS; ++k) {
-        const i64 i = (i64)blockIdx.x * RX_TILE + warp * (RX_ITEMS * 32) + k * 32 + lane;
-        const bool in = i < count;
-        item[k] = in ? radix_item(source, tokens, wide, i, vocab, padding) : make_int2(0, 0);
-        digit[k] = in ? (item[k].x >> shift) & (bins - 1) : -1;
-    }
-    radix_rank<RX_ITEMS>(digit, rank, warp_count[warp], bits);
+    const int rank = radix_rank(digit, warp_count[warp], bits);
     __syncthreads();
     for (int b = tid; b < bins; b += RX_THREADS) {
         int sum = 0;
         for (int w = 0; w < RX_WARPS; ++w) { const int v = warp_count[w][b]; warp_count[w][b] = (unsigned short)sum; sum += v; }
     }
     __syncthreads();
-#pragma unroll
-    for (int k = 0; k < RX_ITEMS; ++k)
-        if (digit[k] >= 0) target[place[digit[k]] + warp_count[warp][digit[k]] + rank[k]] = item[k];
+    if (in) target[place[digit] + warp_count[warp][digit] + rank] = item;
 }
 
 // The run of every token that is there.  (The other entries of runs are never written: who reads one looks whether the position it names holds the token.)
@@ -265,7 +248,7 @@ struct TableShape {
     int accumulate;
     int lanes, slabs;                       // lanes of a team (a power of two); teams side by side that cover a row
     unsigned long_blocks;                   // blocks that add up chunks of long runs; the others form rows
-    int by_run;                             // rows by their runs: only those that tokens name (zeros have been written, or are not wanted)
+    int by_run;                             // rows by their runs: only those that tokens name (zeros have been written, or are not wanted: always where the sums are added to what is there)
 };
 
 template <int VEC> __device__ __forceinline__ void put_floats(float* p, const float (&f)[VEC]) {
@@ -508,7 +491,7 @@ __global__ void __launch_bounds__(ED_SUM_THREADS, MANY || !VECTORS ? 12 : 8) emb
             const int m = run[(r + 1) % ROWS].y - run[(r + 1) % ROWS].x;
             next.fetch(grad + (i64)head[(r + 1) % ROWS].y * s.stride, c, m > 0 && m <= ED_CHUNK);
         }
-        if (first + r >= s.vocab || n > ED_CHUNK || (n == 0 && s.accumulate)) continue;
+        if (first + r >= s.vocab || n > ED_CHUNK) continue;
         if (n > 1) add_run<MANY, T, VEC, VECS>(grad, s.stride, sorted, run[r].x + 1, run[r].y, c, sum);
         put_row<O, VEC, VECS>(out + (first + r) * s.out_stride, c, sum, s);
     }

@@ -103,9 +103,8 @@ size_t policy_layout(void* p, i64 rows, PolicyWork& w) {
 bool valid_rows(i64 rows, i64 length) { return rows >= 0 && length >= 0 && rows <= MOST && length <= MOST; }
 
 struct BalanceBuffers { BalanceWork* work; double* part; float* partial; };
-size_t balance_layout(void* p, i64 rows, i64 experts, BalanceBuffers& w) {
+size_t balance_layout(void* p, i64 experts, BalanceBuffers& w) {
     Sections s(p);
-    (void)rows;
     w.work = s.take<BalanceWork>(1);
     w.part = s.take<double>((size_t)ceil_div(experts, BL_FINISH_COLUMNS));
     w.partial = s.take<float>((size_t)BL_MAX_BLOCKS * (size_t)experts);
@@ -324,7 +323,7 @@ ef21_status ef21_policy_loss(const void* logps_dev, const void* old_dev, const v
 
 size_t ef21_balance_loss_workspace_bytes(int64_t rows, int64_t experts) {
     BalanceBuffers w;
-    return rows < 0 || rows > MOST || experts < 1 || experts > BL_MAX_EXPERTS ? 0 : workspace_size(balance_layout(nullptr, rows, experts, w));
+    return rows < 0 || rows > MOST || experts < 1 || experts > BL_MAX_EXPERTS ? 0 : workspace_size(balance_layout(nullptr, experts, w));
 }
 
 ef21_status ef21_balance_loss(const void* logits_dev, int32_t dtype, int64_t rows, int64_t experts, int64_t logits_stride, const void* choices_dev, int32_t index_type, int64_t chosen,
@@ -338,7 +337,7 @@ ef21_status ef21_balance_loss(const void* logits_dev, int32_t dtype, int64_t row
         return EF21_ERR_INVALID_ARG;
     if (!workspace_fits(workspace_dev, workspace_bytes, need)) return EF21_ERR_WORKSPACE;
     BalanceBuffers w;
-    balance_layout(workspace_dev, rows, experts, w);
+    balance_layout(workspace_dev, experts, w);
     cudaStream_t st = stream_of(cuda_stream);
     return by_dtype(dtype, [&](auto* type) -> ef21_status {
         typedef typename Pointee<decltype(type)>::type T;
