@@ -344,7 +344,9 @@ int64_t ef21_launch_count(const ef21_ctx* ctx);
  * its embedding table and the table's gradient; and, from its logits on, what it is trained on -- log-probabilities of tokens, the
  * logistic loss of paired log ratios (the logistic loss of Section 5 with a pair's log ratio as the margin), a clipped policy loss, and the balance
  * loss of a router that is added to either -- each with its gradient.  Tensors may be fp32, bfloat16 or half; sums, softmax
- * statistics and losses are fp32 or fp64, results are rounded once, in a fixed order: repeated runs agree bit for bit.
+ * statistics and losses are fp32 or fp64, results are rounded once, in a fixed order: repeated runs on
+ * the same arrays agree bit for bit.  (The order in which a row is added up goes by the 16-byte boundaries in it: the same values in a view or a copy of another alignment may
+ * differ in the last bit.)
  * Strides and offsets are in elements, the last dimension is contiguous; no call holds state, and two calls whose workspaces
  * and outputs are not shared may run at the same time.  Device pointers belong to the current device and are
  * multiples of their elements' size.  mask arrays hold one byte per entry: not 0 = counts;

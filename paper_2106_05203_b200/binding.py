@@ -633,7 +633,8 @@ def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, scale: float = 1
     """Log-probabilities of targets[...] under softmax(scale * logits[..., vocab]) -> (logps, lse), fp32, of targets' shape.
 
     logits[rows, vocab] or [batch, length, vocab], with any strides between rows: score whole sequences as
-    token_logprobs(logits[:, :-1], tokens[:, 1:]), no copy is made.  Where the target is `ignore`, the row is not read and both are 0."""
+    token_logprobs(logits[:, :-1], tokens[:, 1:]), no copy is made.  Where the target is `ignore`, the row is not read and both are 0.  The
+    results are constants of autograd; token_logprobs_grad is the backward pass."""
     if stream is None:
         result = _model_calls.token_logprobs(logits, targets, scale, ignore)                        # None: not one of the usual calls
         if result is not None:
@@ -699,7 +700,7 @@ def preference_loss(logps: torch.Tensor, ref_logps: Optional[torch.Tensor] = Non
                     smoothing: float = 0.0, norm: Optional[float] = None, stream: Optional[torch.cuda.Stream] = None) -> PreferenceLoss:
     """Logistic loss of paired log ratios with its gradient: logps[2 P, T] are the log-probabilities of the chosen answers' tokens, then of the rejected
     ones', ref_logps those under the reference (None: 0), mask[2 P, T] the tokens that count (None: all).  The loss is the sum over pairs over `norm`
-    (None: P)."""
+    (None: P).  The results are constants of autograd: logps.backward(result.grad) goes on from here."""
     if stream is None:
         result = _model_calls.preference_loss(logps, ref_logps, mask, beta, smoothing, norm)                        # None: not one of the usual calls
         if result is not None:
@@ -733,7 +734,8 @@ def policy_loss(logps: torch.Tensor, old_logps: torch.Tensor, advantages: torch.
                 reduction: str = "token", norm: Optional[float] = None, stream: Optional[torch.cuda.Stream] = None) -> PolicyLoss:
     """Clipped policy loss with a KL term, with its gradient: logps[R, T], old_logps and ref_logps of the tokens under the policy, the one that drew them, and
     the reference; advantages[R, T] per token, or [R] or [R, 1] per sequence; mask[R, T] the tokens that count (None: all).  reduction "token":
-    all of these weigh the same; "sequence": every row that has any does.  `norm` replaces their number where a step comes in several calls."""
+    all of these weigh the same; "sequence": every row that has any does.  `norm` replaces their number where a step comes in several calls.  The results are constants
+    of autograd: logps.backward(result.grad) goes on from here."""
     if stream is None:
         result = _model_calls.policy_loss(logps, old_logps, advantages, mask, ref_logps, clip_low, clip_high, kl_weight, REDUCTIONS.get(reduction), norm)                        # None: not one of the usual calls
         if result is not None:
@@ -784,7 +786,7 @@ def policy_loss(logps: torch.Tensor, old_logps: torch.Tensor, advantages: torch.
 def balance_loss(logits: torch.Tensor, choices: torch.Tensor, mask: Optional[torch.Tensor] = None, weight: float = 1.0,
                  stream: Optional[torch.cuda.Stream] = None) -> BalanceLoss:
     """Balance loss of a router, tokens per expert, and the gradient of the router's logits[R, E]: choices[R, K] are the experts that each token goes to
-    (one outside [0, E) counts for none), mask[R] the tokens that count (None: all)."""
+    (one outside [0, E) counts for none), mask[R] the tokens that count (None: all).  The results are constants of autograd: logits.backward(result.grad) goes on from here."""
     if stream is None:
         result = _model_calls.balance_loss(logits, choices, mask, weight)                        # None: not one of the usual calls
         if result is not None:
@@ -818,7 +820,8 @@ def balance_loss(logits: torch.Tensor, choices: torch.Tensor, mask: Optional[tor
 
 
 def embedding(weight: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-    """scale * weight[tokens] -> [*tokens.shape, dim]; a token outside the table reads as zeros (as where a table is split by rows)."""
+    """scale * weight[tokens] -> [*tokens.shape, dim]; a token outside the table reads as zeros (as where a table is split by rows).  The
+    result is a constant of autograd; embedding_grad is the backward pass."""
     if stream is None:
         result = _model_calls.embedding(weight, tokens, scale)                        # None: not one of the usual calls
         if result is not None:

@@ -8,7 +8,8 @@
 // counting for itself.  f is taken about its mean: f_e - 1/E = (counts_e E - K N) / (K N E), exact in whole numbers, since the sum over p takes a constant away -- a
 // balanced router has small differences of shares that are alike.
 //
-// 131,072 x 256 bf16, 8 chosen: 39 us, of which the pass 30 (140 instructions per row and warp at 0.6 of the issue slots, 16 lanes a row; 32 lanes a row: 200 and 40 us); 512 x 8: 8.5 us, a launch.
+// 131,072 x 256 bf16, 8 chosen: 40 us, of which the pass 32 by itself (140 instructions per row and warp at 0.59 of the issue slots, 16 lanes a row; 32 lanes a row: 218 and 45 us); 512 x 8: 8.6 us, a
+// launch.  Rows that are no whole aligned vectors move element by element, each with its own bound check: 100,000 x 255 bf16 85 us, five times its bytes.
 #pragma once
 #include "cluster.cuh"
 #include "element.cuh"

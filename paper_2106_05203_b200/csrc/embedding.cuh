@@ -7,9 +7,10 @@
 // has at most ED_CHUNK positions is formed by the lanes of one team and written once, zeros where no token names it, while other blocks of the same
 // launch add up the longer runs ED_CHUNK sorted positions at a time; a last launch joins these sums, in order.
 //
-// Lookup of 16,384 x 4,096 bf16: 32.5 us, 5.9 TB/s.  Gradient of 65,536 tokens (the most frequent 6,000 times) into 50,257 x 2,048 fp32: 167 us; the sums 130 (700 MB), the sort
-// in front of them 24, the join behind them 8.  1,000 tokens into 1,024 x 257 fp32: 10 us; 3,000 into 10,000 x 64 half 18,
-// 8,000 into 500 x 40 bf16 25 (24 and 28 with two positions in flight, as large tables have).
+// Lookup of 16,384 x 4,096 bf16: 32.5 us, 5.9 TB/s.  Gradient of 65,536 tokens (the most frequent 6,000 times) into 50,257 x 2,048 fp32: 167 us as
+// dependent launches; each by itself, caches warm: the seven of the sort 39, the sums 138 (269 MB read, 373 written while it runs: 4.7 TB/s; 80 registers, 44 / 84 bytes of spills), the
+// join 15.  1,000 tokens into 1,024 x 257 fp32: 10.5 us; 3,000 into 10,000 x 64 half 19, 8,000 into 500 x 40 bf16 23 (24 and 28 with two positions in flight, as large tables
+// have).  Rows that are no whole vectors move by single elements: 60,000 bf16 tokens into 98,621 x 917 fp32 425, six times its bytes.
 //
 // Sorting: up to ED_RANK_TOKENS tokens by counting, for every token, those in front of it -- one launch; more by a radix sort, digits of up to nine bits, three launches
 // each.  (All passes in the shared memory of one cluster were measured, too: 4 us faster at 9,000 tokens, as fast at 30,000, 10 us slower at 65,000.)

@@ -77,7 +77,7 @@ i64 logprob_units(int32_t dtype, i64 rows, i64 vocab) {
 // ---- preference loss: which kernel --------------------------------------------------------------------------------------------------------
 
 // Blocks per pair: one where the pairs fill the device, up to eight of at least PF_PART elements each where they do not.  (A cluster's barriers cost: 512 pairs x
-// 8,191 fp32 by one block each 24 us, by eight 40.)
+// 8,191 fp32 by one block each 22 us, by eight 52; replayed from a graph.)
 struct PreferencePlan { bool by_warp, one; unsigned split, blocks; i64 losses; };
 PreferencePlan preference_plan(i64 pairs, i64 length) {
     PreferencePlan p;

@@ -4,7 +4,7 @@
 //   loss = 1/N sum_p [ -(1 - eps) log sigma(z_p) - eps log sigma(-z_p) ]
 //   d loss / d lp_rt = -+ beta/N (sigma(-z_p) - eps) m_rt       (minus: chosen row p; plus: rejected row P + p)
 //
-// 512 pairs x 8,191 fp32: 20.5 us, 5.3 TB/s of what is there (4.1 of what is read and written), two reductions between reading and writing; 4 pairs x 512: 6.6 us, a launch.
+// 512 pairs x 8,191 fp32: 20.6 us, 5.3 TB/s of what is there (4.1 of what is read and written), two reductions between reading and writing; 4 pairs x 512: 6.9 us, a launch.
 //
 // What the mask leaves out is not read; the gradient -- one value per row -- is written where it holds.  Short rows: a warp has a pair, a block eight.  Longer
 // ones: a pair has one block, or up to eight that form a cluster and add up their sums; PF_PART elements are one vector of 16 bytes (fp32) per thread, so that both rows'
